@@ -316,6 +316,152 @@ int cascade_measure_ceilings(void* dev_buffer, size_t bytes, void* stream, casca
 /* Text of the last error of this context (or of the last failed cascade_init if ctx is NULL). */
 const char* cascade_last_error(const cascade_ctx* ctx);
 
+/* ------------------------------------------------------------------------------------------------
+ * Norms of queries and keys, and a paged cache held in 4 bits.
+ *
+ * Models that mix layers with a cascading cache and layers that keep every token, or that normalise
+ * queries and keys per head, need the three steps below next to the calls above.  They share the
+ * conventions at the top of this file; differences are named at the call.
+ */
+
+/*
+ * Rotation table: cosines and sines of p * theta_i, theta_i = base^(-2i/d), for positions
+ * 0 <= p < n_positions, as two tables in 64 bits (every 256th position, and 256 offsets) whose
+ * entries are combined by the angle sum: 4.5 MB for a million positions at head_dim 128, exact to the
+ * last bits of a float.  The buffer is the caller's, 16-byte aligned, and may be shared by all calls that
+ * take dev_rope, on any number of contexts.
+ *   cascade_rope_table_bytes: size of the buffer; 0 for arguments out of range (head_dim even and 2 to 256,
+ *     1 <= n_positions <= 2^31).
+ * Errors: NULL_ARG, BAD_ARG (range, alignment, base not above 0), WORKSPACE_TOO_SMALL, HIP.
+ */
+size_t cascade_rope_table_bytes(int64_t n_positions, int32_t head_dim);
+int cascade_rope_table(void* dev_rope, size_t bytes, int64_t n_positions, int32_t head_dim, float base, void* stream);
+
+/*
+ * Per-head RMS norm of queries and keys with the rotation in the same pass, for every row x of head_dim values:
+ *   y = x / sqrt(mean(x^2) + eps) * weight      (norm = 1; a NULL weight stands for ones)
+ *   (y_i, y_{i+d/2}) turned by p * theta_i       (dev_positions given)
+ * in 32 bits, rounded once to the element type.  With dev_positions NULL nothing is rotated, which is what
+ * cascade_prefill_chunk and cascade_decode_step take (they rotate by cache index themselves).
+ * Rows: [n_tokens, heads, head_dim], heads contiguous, tokens `*_stride` elements apart (0: heads * head_dim), so
+ * that views of a fused projection can be passed.  An output may be its own input with the same stride; it must not
+ * overlap an input in any other way.  n_k_heads = 0 or n_q_heads = 0 leaves that part out; n_tokens = 0 does nothing.
+ * A position outside [0, rope_positions) gives rows of NaN.
+ * Any even head_dim from 2 to 256; rows of whole 16-byte pieces at 16-byte aligned places (head_dim a multiple of 16)
+ * take the fast form.
+ * Errors (text: cascade_last_error(NULL)): NULL_ARG, UNSUPPORTED (dtype, head_dim), BAD_ARG, HIP.
+ */
+typedef struct cascade_norm_rope_args {
+    int32_t dtype;             /* CASCADE_F32 or CASCADE_BF16: q, k, outputs and weights */
+    int32_t head_dim;
+    int32_t n_tokens;
+    int32_t n_q_heads, n_k_heads;
+    int32_t norm;              /* 1: normalise; 0: rotation only */
+    float eps;                 /* >= 0 */
+    int32_t reserved;          /* 0 */
+    const void* dev_q;
+    const void* dev_k;
+    void* dev_q_out;
+    void* dev_k_out;
+    int64_t q_stride, k_stride, q_out_stride, k_out_stride;
+    const void* dev_q_weight;  /* [head_dim] or NULL */
+    const void* dev_k_weight;
+    const int32_t* dev_positions;   /* [n_tokens] or NULL */
+    const void* dev_rope;      /* cascade_rope_table for this head_dim; needed with dev_positions */
+    int64_t rope_positions;    /* positions of that table */
+} cascade_norm_rope_args;
+int cascade_norm_rope(const cascade_norm_rope_args* args, void* stream);
+
+/*
+ * A paged cache of keys and values in 4 bits, for attention over every token of a sequence.  A page holds page_size
+ * consecutive tokens of one sequence for all KV heads; pages, page tables and lengths are the caller's, so that
+ * sequences can share pages and a pool can hand them out in any order.
+ *
+ * Numbers: a code is a sign bit over three bits that stand for 0, 0.5, 1, 1.5, 2, 3, 4, 6 (to the nearest, ties to the even code).
+ *   K: every 32 channels of a row have the scale 2^e, e the smallest whole number (-126 .. 127) with max|k| <= 7 * 2^e
+ *      (7 is the largest value that still rounds to 6), stored as the byte e + 127; all zeros: byte 0.
+ *   V: a row has the scale s = max|v| / 6 rounded to bf16; values are code * s.
+ *   A K block or V row with an infinity or NaN becomes NaN as a whole (exponent byte 255, scale NaN); a V row with s below
+ *   2^-100 becomes zero.
+ *   What is stored for a token depends on its row and its position alone, not on the call, chunk or kernel that wrote it.
+ * Bytes: a page is [n_kv_heads][page_size / 32] groups of 32 tokens of (33 * head_dim + 64) bytes, rounded up to 128.
+ * Token r of a group, channel c:
+ *   K codes at 0:           byte (c/32)*512 + r*16 + (c%32)/2, low four bits for even c
+ *   V codes at 16*head_dim: byte (c/64)*1024 + ((r/4)%4)*256 + (c%16)*16 + ((c/32)%2)*8 + (r/16)*4 + r%4, low four bits where c/16 is even
+ *   K bytes at 32*head_dim: byte (c/32)*32 + (r%16)*2 + r/16
+ *   V scales at 33*head_dim: bf16 number ((r/4)%4)*8 + (r/16)*4 + r%4
+ */
+typedef struct cascade_paged_config {
+    int32_t n_q_heads;         /* a multiple of n_kv_heads */
+    int32_t n_kv_heads;
+    int32_t head_dim;          /* 64 or 128 */
+    int32_t dtype;             /* CASCADE_F32 or CASCADE_BF16: q, k, v and outputs */
+    int32_t page_size;         /* a multiple of 32, at most 65536 */
+    int32_t max_seqs;          /* largest n_seqs of a batch, at most 65536 */
+    int64_t n_pages;           /* pages in dev_pages */
+    float softmax_scale;       /* 0 selects 1/sqrt(head_dim) */
+    int32_t window;            /* 0: a query sees every token up to its own; w > 0: the last w of them */
+} cascade_paged_config;
+
+/*
+ * The sequences of one call.  Sequence s has dev_lengths[s] tokens in the cache and dev_new_offsets[s+1] - dev_new_offsets[s]
+ * new ones, which are rows dev_new_offsets[s] ... of the call's token arrays, at positions dev_lengths[s], dev_lengths[s] + 1, ...
+ * Position p lies in page dev_page_table[s * table_stride + p / page_size].  All four arrays are read by the kernels when they run (a captured
+ * graph sees what they hold at replay); n_tokens, max_new and max_length are what the host knows, and must bound what the arrays hold.
+ * What goes beyond them is left out: tokens from row n_tokens on are neither written nor attended from, positions at or above max_length,
+ * behind the end of the table or on a page outside [0, n_pages) are neither written nor seen.
+ * Two new tokens on the same slot of the same page (a page listed twice): one of them is stored, or parts of both.
+ */
+typedef struct cascade_paged_batch {
+    int32_t n_seqs;
+    int32_t n_tokens;                  /* rows of the call's token arrays: dev_new_offsets[n_seqs] */
+    int32_t max_new;                   /* no sequence has more new tokens */
+    int32_t max_length;                /* no sequence is longer, new tokens included */
+    const int32_t* dev_lengths;        /* [n_seqs] tokens before the new ones */
+    const int32_t* dev_new_offsets;    /* [n_seqs + 1], ascending from 0 */
+    const int32_t* dev_page_table;     /* [n_seqs, table_stride] */
+    int64_t table_stride;              /* pages a sequence can list */
+} cascade_paged_batch;
+
+typedef struct cascade_paged_ctx cascade_paged_ctx;
+
+/* Bytes of one page, and of the workspace of a context; 0 if the configuration is invalid. */
+size_t cascade_paged_page_bytes(const cascade_paged_config* cfg);
+size_t cascade_paged_workspace_bytes(const cascade_paged_config* cfg);
+
+/*
+ * A context on the current device.  dev_pages: n_pages * cascade_paged_page_bytes bytes, 128-byte aligned; their contents are left
+ * as they are (pages of an earlier context, or unwritten memory: what no sequence's length reaches is never seen).  dev_workspace: 256-byte aligned,
+ * holds partial results within a call; contexts may share one where their calls are ordered with each other, and so may graphs.
+ * dev_rope, rope_positions: a table of cascade_rope_table for head_dim, or NULL, 0: append then stores keys as they come.
+ * Nothing is launched.  Errors: NULL_ARG, INVALID_CONFIG, UNSUPPORTED, WORKSPACE_TOO_SMALL, BAD_ARG (alignment), HIP.
+ */
+int cascade_paged_init(const cascade_paged_config* cfg, void* dev_pages, void* dev_workspace, size_t workspace_bytes,
+                       const void* dev_rope, int64_t rope_positions, cascade_paged_ctx** out_ctx);
+void cascade_paged_destroy(cascade_paged_ctx* ctx);
+
+/*
+ * The three calls below read the batch's arrays and return at once; they can be captured into a graph.  Token arrays are
+ * [n_tokens, heads, head_dim], heads contiguous, tokens `*_stride` elements apart (0: heads * head_dim), 16-byte aligned with strides of
+ * whole 16-byte pieces.  n_tokens = 0 or n_seqs = 0 does nothing.  The calls advance no length: the caller does once all of a step are issued.
+ * Errors: NULL_ARG, BAD_ARG, HIP.
+ *
+ * append: keys (rotated to their positions if the context has a table) and values of the new tokens into the pages.  dev_q (may be NULL):
+ *   their queries, rotated in the same launch into dev_q_out [n_tokens, n_q_heads, head_dim], rounded to the element type (dev_q_out may be
+ *   dev_q if that is contiguous); needs the table.
+ * attend: dev_out[t] = softmax attention of query t (already rotated) over its sequence's positions up to its own (within the window).
+ *   The new tokens' keys have to be in the cache (append).  A query that sees nothing gives zeros.
+ * read: the new tokens' rows as the values they stand for, into contiguous dev_k_out and dev_v_out (either may be NULL); a row that was left out
+ *   on writing (see cascade_paged_batch) is read as zeros.  Any range of a sequence can be read by a batch that calls it new.
+ */
+int cascade_paged_append(cascade_paged_ctx* ctx, const cascade_paged_batch* batch, const void* dev_k, int64_t k_stride, const void* dev_v, int64_t v_stride,
+                         const void* dev_q, int64_t q_stride, void* dev_q_out, void* stream);
+int cascade_paged_attend(cascade_paged_ctx* ctx, const cascade_paged_batch* batch, const void* dev_q, int64_t q_stride, void* dev_out, void* stream);
+int cascade_paged_read(cascade_paged_ctx* ctx, const cascade_paged_batch* batch, void* dev_k_out, void* dev_v_out, void* stream);
+
+/* Text of the last error of this context (of the last failed cascade_paged_init if ctx is NULL). */
+const char* cascade_paged_last_error(const cascade_paged_ctx* ctx);
+
 #ifdef __cplusplus
 }
 #endif

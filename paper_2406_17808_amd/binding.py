@@ -37,6 +37,9 @@ EXPORTED_SYMBOLS = [
     "cascade_decode_step", "cascade_read_state", "cascade_simulate_structure", "cascade_last_error",
     "cascade_profile_begin", "cascade_profile_end", "cascade_layers_workspace_bytes", "cascade_init_layers",
     "cascade_init_static", "cascade_measure_ceilings", "cascade_profile_begin_families",
+    "cascade_rope_table_bytes", "cascade_rope_table", "cascade_norm_rope",
+    "cascade_paged_page_bytes", "cascade_paged_workspace_bytes", "cascade_paged_init", "cascade_paged_destroy",
+    "cascade_paged_append", "cascade_paged_attend", "cascade_paged_read", "cascade_paged_last_error",
 ]
 CASCADE_STATIC_WORKSPACE_BYTES = 64 << 20
 
@@ -102,6 +105,34 @@ class cascade_profile(ctypes.Structure):
     _fields_ = [("ms", ctypes.c_double * CASCADE_K_FAMILIES), ("intervals", ctypes.c_int64 * CASCADE_K_FAMILIES)]
 
 
+class cascade_norm_rope_args(ctypes.Structure):
+    _fields_ = [
+        ("dtype", ctypes.c_int32), ("head_dim", ctypes.c_int32), ("n_tokens", ctypes.c_int32),
+        ("n_q_heads", ctypes.c_int32), ("n_k_heads", ctypes.c_int32), ("norm", ctypes.c_int32),
+        ("eps", ctypes.c_float), ("reserved", ctypes.c_int32),
+        ("dev_q", ctypes.c_void_p), ("dev_k", ctypes.c_void_p), ("dev_q_out", ctypes.c_void_p), ("dev_k_out", ctypes.c_void_p),
+        ("q_stride", ctypes.c_int64), ("k_stride", ctypes.c_int64), ("q_out_stride", ctypes.c_int64), ("k_out_stride", ctypes.c_int64),
+        ("dev_q_weight", ctypes.c_void_p), ("dev_k_weight", ctypes.c_void_p),
+        ("dev_positions", ctypes.c_void_p), ("dev_rope", ctypes.c_void_p), ("rope_positions", ctypes.c_int64),
+    ]
+
+
+class cascade_paged_config(ctypes.Structure):
+    _fields_ = [
+        ("n_q_heads", ctypes.c_int32), ("n_kv_heads", ctypes.c_int32), ("head_dim", ctypes.c_int32), ("dtype", ctypes.c_int32),
+        ("page_size", ctypes.c_int32), ("max_seqs", ctypes.c_int32), ("n_pages", ctypes.c_int64),
+        ("softmax_scale", ctypes.c_float), ("window", ctypes.c_int32),
+    ]
+
+
+class cascade_paged_batch(ctypes.Structure):
+    _fields_ = [
+        ("n_seqs", ctypes.c_int32), ("n_tokens", ctypes.c_int32), ("max_new", ctypes.c_int32), ("max_length", ctypes.c_int32),
+        ("dev_lengths", ctypes.c_void_p), ("dev_new_offsets", ctypes.c_void_p), ("dev_page_table", ctypes.c_void_p),
+        ("table_stride", ctypes.c_int64),
+    ]
+
+
 _LIB = None
 
 
@@ -144,6 +175,28 @@ def load_library():
         L.cascade_profile_end.argtypes = [P, ctypes.POINTER(cascade_profile)]
         L.cascade_measure_ceilings.restype = ctypes.c_int
         L.cascade_measure_ceilings.argtypes = [P, ctypes.c_size_t, P, ctypes.POINTER(cascade_ceilings)]
+        I64 = ctypes.c_int64
+        L.cascade_rope_table_bytes.restype = ctypes.c_size_t
+        L.cascade_rope_table_bytes.argtypes = [I64, ctypes.c_int32]
+        L.cascade_rope_table.restype = ctypes.c_int
+        L.cascade_rope_table.argtypes = [P, ctypes.c_size_t, I64, ctypes.c_int32, ctypes.c_float, P]
+        L.cascade_norm_rope.restype = ctypes.c_int
+        L.cascade_norm_rope.argtypes = [ctypes.POINTER(cascade_norm_rope_args), P]
+        for name in ("cascade_paged_page_bytes", "cascade_paged_workspace_bytes"):
+            getattr(L, name).restype = ctypes.c_size_t
+            getattr(L, name).argtypes = [ctypes.POINTER(cascade_paged_config)]
+        L.cascade_paged_init.restype = ctypes.c_int
+        L.cascade_paged_init.argtypes = [ctypes.POINTER(cascade_paged_config), P, P, ctypes.c_size_t, P, I64, ctypes.POINTER(P)]
+        L.cascade_paged_destroy.restype = None
+        L.cascade_paged_destroy.argtypes = [P]
+        L.cascade_paged_append.restype = ctypes.c_int
+        L.cascade_paged_append.argtypes = [P, ctypes.POINTER(cascade_paged_batch), P, I64, P, I64, P, I64, P, P]
+        L.cascade_paged_attend.restype = ctypes.c_int
+        L.cascade_paged_attend.argtypes = [P, ctypes.POINTER(cascade_paged_batch), P, I64, P, P]
+        L.cascade_paged_read.restype = ctypes.c_int
+        L.cascade_paged_read.argtypes = [P, ctypes.POINTER(cascade_paged_batch), P, P, P]
+        L.cascade_paged_last_error.restype = ctypes.c_char_p
+        L.cascade_paged_last_error.argtypes = [P]
         L.cascade_last_error.restype = ctypes.c_char_p
         L.cascade_last_error.argtypes = [P]
         _LIB = L
@@ -341,3 +394,61 @@ def cascade_simulate_structure(cfg: cascade_config, chunk_sizes: Sequence[int],
     _check(rc, None)
     return StateArrays(view, N, None if ids is None else ids[:slots], None if mu is None else mu[:slots],
                        slot[:slots], None, None, swaps)
+
+
+def make_paged_config(n_q_heads: int, n_kv_heads: int, head_dim: int, dtype: int, page_size: int, n_pages: int, max_seqs: int,
+                      softmax_scale: float = 0.0, window: int = 0) -> cascade_paged_config:
+    return cascade_paged_config(n_q_heads=n_q_heads, n_kv_heads=n_kv_heads, head_dim=head_dim, dtype=dtype, page_size=page_size,
+                                max_seqs=max_seqs, n_pages=n_pages, softmax_scale=softmax_scale, window=window)
+
+
+def _check_paged(rc: int, ctx) -> None:
+    if rc != CASCADE_OK:
+        msg = load_library().cascade_paged_last_error(ctx)
+        raise CascadeError(rc, msg.decode() if msg else "")
+
+
+def cascade_rope_table_bytes(n_positions: int, head_dim: int) -> int:
+    return int(load_library().cascade_rope_table_bytes(n_positions, head_dim))
+
+
+def cascade_rope_table(dev_rope: int, nbytes: int, n_positions: int, head_dim: int, base: float, stream: int = 0) -> None:
+    _check(load_library().cascade_rope_table(dev_rope, nbytes, n_positions, head_dim, base, stream), None)
+
+
+def cascade_norm_rope(args: cascade_norm_rope_args, stream: int = 0) -> None:
+    _check(load_library().cascade_norm_rope(ctypes.byref(args), stream), None)
+
+
+def cascade_paged_page_bytes(cfg: cascade_paged_config) -> int:
+    return int(load_library().cascade_paged_page_bytes(ctypes.byref(cfg)))
+
+
+def cascade_paged_workspace_bytes(cfg: cascade_paged_config) -> int:
+    return int(load_library().cascade_paged_workspace_bytes(ctypes.byref(cfg)))
+
+
+def cascade_paged_init(cfg: cascade_paged_config, dev_pages: int, dev_workspace: int, workspace_bytes: int, dev_rope: int = 0,
+                       rope_positions: int = 0) -> ctypes.c_void_p:
+    ctx = ctypes.c_void_p()
+    _check_paged(load_library().cascade_paged_init(ctypes.byref(cfg), dev_pages, dev_workspace, workspace_bytes, dev_rope or None,
+                                                   rope_positions, ctypes.byref(ctx)), None)
+    return ctx
+
+
+def cascade_paged_destroy(ctx) -> None:
+    load_library().cascade_paged_destroy(ctx)
+
+
+def cascade_paged_append(ctx, batch: cascade_paged_batch, dev_k: int, k_stride: int, dev_v: int, v_stride: int, dev_q: int = 0, q_stride: int = 0,
+                         dev_q_out: int = 0, stream: int = 0) -> None:
+    _check_paged(load_library().cascade_paged_append(ctx, ctypes.byref(batch), dev_k, k_stride, dev_v, v_stride, dev_q or None, q_stride,
+                                                     dev_q_out or None, stream), ctx)
+
+
+def cascade_paged_attend(ctx, batch: cascade_paged_batch, dev_q: int, q_stride: int, dev_out: int, stream: int = 0) -> None:
+    _check_paged(load_library().cascade_paged_attend(ctx, ctypes.byref(batch), dev_q, q_stride, dev_out, stream), ctx)
+
+
+def cascade_paged_read(ctx, batch: cascade_paged_batch, dev_k_out: int = 0, dev_v_out: int = 0, stream: int = 0) -> None:
+    _check_paged(load_library().cascade_paged_read(ctx, ctypes.byref(batch), dev_k_out or None, dev_v_out or None, stream), ctx)

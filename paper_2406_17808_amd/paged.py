@@ -1,0 +1,172 @@
+"""Norms of queries and keys per head, and a paged cache held in 4 bits, for callers that hold torch tensors.
+
+Like cache.py this owns device memory and passes data pointers and the current stream to the C ABI; no arithmetic
+happens here.
+"""
+from __future__ import annotations
+
+from typing import Optional, Tuple
+
+import torch
+
+from . import binding as B
+
+_TYPES = {torch.bfloat16: B.CASCADE_BF16, torch.float32: B.CASCADE_F32}
+
+
+def _stream(device: torch.device) -> int:
+    return torch.cuda.current_stream(device).cuda_stream
+
+
+def _check_rows(x: torch.Tensor, device, dtype, heads: int, head_dim: int, tokens: Optional[int] = None) -> None:
+    """[tokens, heads, head_dim] with the heads of a token next to each other; tokens may lie further apart."""
+    assert x.is_cuda and x.device == device and x.dtype == dtype and x.dim() == 3, (x.device, x.dtype, tuple(x.shape))
+    assert x.shape[1:] == (heads, head_dim) and (tokens is None or x.shape[0] == tokens), (tuple(x.shape), tokens, heads, head_dim)
+    assert x.numel() == 0 or ((x.stride(2) == 1 or head_dim == 1) and (x.stride(1) == head_dim or heads == 1)), x.stride()
+
+
+def _row_stride(x: torch.Tensor) -> int:
+    return x.stride(0) if x.shape[0] > 1 else 0      # the stride of a single token says nothing
+
+
+class RopeTable:
+    """Cosines and sines of the positions below n_positions (pairs (i, i + head_dim / 2), angles p * base^(-2i / head_dim))."""
+
+    def __init__(self, n_positions: int, head_dim: int, base: float, device: str = "cuda:0"):
+        self.n_positions, self.head_dim, self.base = n_positions, head_dim, base
+        self.device = torch.device(device)
+        nbytes = B.cascade_rope_table_bytes(n_positions, head_dim)
+        self.table = torch.empty(max(nbytes, 16), dtype=torch.uint8, device=self.device)
+        with torch.cuda.device(self.device):
+            B.cascade_rope_table(self.table.data_ptr(), nbytes, n_positions, head_dim, base, _stream(self.device))
+
+
+def qk_norm_rope(q: torch.Tensor, k: Optional[torch.Tensor] = None, q_weight: Optional[torch.Tensor] = None,
+                 k_weight: Optional[torch.Tensor] = None, eps: float = 1e-6, norm: bool = True, positions: Optional[torch.Tensor] = None,
+                 rope: Optional[RopeTable] = None, q_out: Optional[torch.Tensor] = None,
+                 k_out: Optional[torch.Tensor] = None) -> Tuple[torch.Tensor, Optional[torch.Tensor]]:
+    """RMS norm over head_dim of q [tokens, q heads, head_dim] and k [tokens, k heads, head_dim] with the rotation to `positions`
+    [tokens] (int32; None: not rotated, as CascadeKVCache takes them) in the same pass.  norm=False rotates only.  Tokens
+    of q and k may lie apart (views of a fused projection).  q_out / k_out may be q / k."""
+    device, dtype, (tokens, hq, d) = q.device, q.dtype, q.shape
+    assert dtype in _TYPES, dtype
+    _check_rows(q, device, dtype, hq, d)
+    a = B.cascade_norm_rope_args(dtype=_TYPES[dtype], head_dim=d, n_tokens=tokens, n_q_heads=hq, norm=int(norm), eps=eps)
+    if q_out is None:
+        q_out = torch.empty((tokens, hq, d), dtype=dtype, device=device)
+    _check_rows(q_out, device, dtype, hq, d, tokens)
+    a.dev_q, a.dev_q_out, a.q_stride, a.q_out_stride = q.data_ptr(), q_out.data_ptr(), _row_stride(q), _row_stride(q_out)
+    if k is not None:
+        hk = k.shape[1]
+        _check_rows(k, device, dtype, hk, d, tokens)
+        if k_out is None:
+            k_out = torch.empty((tokens, hk, d), dtype=dtype, device=device)
+        _check_rows(k_out, device, dtype, hk, d, tokens)
+        a.n_k_heads = hk
+        a.dev_k, a.dev_k_out, a.k_stride, a.k_out_stride = k.data_ptr(), k_out.data_ptr(), _row_stride(k), _row_stride(k_out)
+    else:
+        assert k_out is None and k_weight is None
+    for w in (q_weight, k_weight):
+        assert w is None or (norm and w.device == device and w.dtype == dtype and tuple(w.shape) == (d,) and w.is_contiguous())
+    a.dev_q_weight = q_weight.data_ptr() if q_weight is not None else None
+    a.dev_k_weight = k_weight.data_ptr() if k_weight is not None else None
+    if positions is not None:
+        assert positions.device == device and positions.dtype == torch.int32 and tuple(positions.shape) == (tokens,) and positions.is_contiguous()
+        assert rope is not None and rope.device == device and rope.head_dim == d, "positions need a RopeTable of this head_dim"
+        a.dev_positions, a.dev_rope, a.rope_positions = positions.data_ptr(), rope.table.data_ptr(), rope.n_positions
+    with torch.cuda.device(device):
+        B.cascade_norm_rope(a, _stream(device))
+    return q_out, k_out
+
+
+class PagedBatch:
+    """The sequences of one call (see cascade_paged_batch): lengths [n] tokens before the new ones, new_offsets [n + 1] rows of the new tokens,
+    page_table [n, pages], int32 on the device, and the host's bounds on what they hold.  The arrays are read when the kernels run, so a
+    captured step follows lengths that are advanced in place."""
+
+    def __init__(self, lengths: torch.Tensor, new_offsets: torch.Tensor, page_table: torch.Tensor, n_tokens: int, max_new: int, max_length: int):
+        n = lengths.shape[0]
+        for x in (lengths, new_offsets, page_table):
+            assert x.is_cuda and x.dtype == torch.int32 and x.device == lengths.device, (x.device, x.dtype)
+        assert lengths.dim() == 1 and lengths.is_contiguous() and tuple(new_offsets.shape) == (n + 1,) and new_offsets.is_contiguous()
+        assert page_table.dim() == 2 and page_table.shape[0] == n and page_table.is_contiguous()
+        self.lengths, self.new_offsets, self.page_table = lengths, new_offsets, page_table
+        self.n_tokens, self.max_new, self.max_length = int(n_tokens), int(max_new), int(max_length)
+        self.c = B.cascade_paged_batch(n_seqs=n, n_tokens=self.n_tokens, max_new=self.max_new, max_length=self.max_length,
+                                       dev_lengths=lengths.data_ptr(), dev_new_offsets=new_offsets.data_ptr(),
+                                       dev_page_table=page_table.data_ptr(), table_stride=page_table.shape[1])
+
+
+class PagedKVCache:
+    """Pages of keys and values in 4 bits (see cascade_paged_config for the numbers and bytes).  `pages` [n_pages, page bytes] uint8 may be handed in;
+    with `rope` append rotates keys, and the queries given to it, to their positions."""
+
+    def __init__(self, cfg: B.cascade_paged_config, device: str = "cuda:0", pages: Optional[torch.Tensor] = None, rope: Optional[RopeTable] = None):
+        self.cfg, self.rope = cfg, rope
+        self.device = torch.device(device)
+        self.torch_dtype = torch.bfloat16 if cfg.dtype == B.CASCADE_BF16 else torch.float32
+        self.page_bytes = B.cascade_paged_page_bytes(cfg)
+        self.workspace_bytes = B.cascade_paged_workspace_bytes(cfg)
+        if self.workspace_bytes == 0:
+            B.cascade_paged_init(cfg, 256, 256, 0)      # reports why
+        if pages is None:
+            pages = torch.empty((cfg.n_pages, self.page_bytes), dtype=torch.uint8, device=self.device)
+        assert pages.device == self.device and pages.dtype == torch.uint8 and tuple(pages.shape) == (cfg.n_pages, self.page_bytes) and pages.is_contiguous()
+        assert rope is None or (rope.device == self.device and rope.head_dim == cfg.head_dim)
+        self.pages = pages
+        self.workspace = torch.empty(self.workspace_bytes + 256, dtype=torch.uint8, device=self.device)
+        with torch.cuda.device(self.device):
+            self.ctx = B.cascade_paged_init(cfg, pages.data_ptr(), (self.workspace.data_ptr() + 255) & ~255, self.workspace_bytes,
+                                            rope.table.data_ptr() if rope is not None else 0, rope.n_positions if rope is not None else 0)
+
+    def close(self):
+        if getattr(self, "ctx", None):
+            torch.cuda.synchronize(self.device)
+            B.cascade_paged_destroy(self.ctx)
+            self.ctx = None
+
+    def __del__(self):
+        try:
+            self.close()
+        except Exception:
+            pass
+
+    def append(self, batch: PagedBatch, k: torch.Tensor, v: torch.Tensor, q: Optional[torch.Tensor] = None,
+               q_out: Optional[torch.Tensor] = None) -> Optional[torch.Tensor]:
+        """Stores k, v [n_tokens, kv heads, head_dim] of the batch's new tokens; q [n_tokens, q heads, head_dim] is rotated into q_out, which is returned."""
+        c = self.cfg
+        assert batch.lengths.device == self.device
+        _check_rows(k, self.device, self.torch_dtype, c.n_kv_heads, c.head_dim, batch.n_tokens)
+        _check_rows(v, self.device, self.torch_dtype, c.n_kv_heads, c.head_dim, batch.n_tokens)
+        if q is not None:
+            _check_rows(q, self.device, self.torch_dtype, c.n_q_heads, c.head_dim, batch.n_tokens)
+            if q_out is None:
+                q_out = torch.empty((batch.n_tokens, c.n_q_heads, c.head_dim), dtype=self.torch_dtype, device=self.device)
+            _check_rows(q_out, self.device, self.torch_dtype, c.n_q_heads, c.head_dim, batch.n_tokens)
+            assert q_out.is_contiguous()
+        else:
+            assert q_out is None
+        B.cascade_paged_append(self.ctx, batch.c, k.data_ptr(), _row_stride(k), v.data_ptr(), _row_stride(v),
+                               q.data_ptr() if q is not None else 0, _row_stride(q) if q is not None else 0,
+                               q_out.data_ptr() if q is not None else 0, _stream(self.device))
+        return q_out
+
+    def attend(self, batch: PagedBatch, q: torch.Tensor, out: Optional[torch.Tensor] = None) -> torch.Tensor:
+        """Attention of q [n_tokens, q heads, head_dim], rotated, over the cache, the batch's new tokens included."""
+        c = self.cfg
+        assert batch.lengths.device == self.device
+        _check_rows(q, self.device, self.torch_dtype, c.n_q_heads, c.head_dim, batch.n_tokens)
+        if out is None:
+            out = torch.empty((batch.n_tokens, c.n_q_heads, c.head_dim), dtype=self.torch_dtype, device=self.device)
+        _check_rows(out, self.device, self.torch_dtype, c.n_q_heads, c.head_dim, batch.n_tokens)
+        assert out.is_contiguous()
+        B.cascade_paged_attend(self.ctx, batch.c, q.data_ptr(), _row_stride(q), out.data_ptr(), _stream(self.device))
+        return out
+
+    def read(self, batch: PagedBatch) -> Tuple[torch.Tensor, torch.Tensor]:
+        """The rows that the batch calls new, as the values their codes stand for."""
+        c = self.cfg
+        assert batch.lengths.device == self.device
+        k, v = (torch.empty((batch.n_tokens, c.n_kv_heads, c.head_dim), dtype=self.torch_dtype, device=self.device) for _ in range(2))
+        B.cascade_paged_read(self.ctx, batch.c, k.data_ptr(), v.data_ptr(), _stream(self.device))
+        return k, v
