@@ -397,7 +397,7 @@ typedef struct cascade_paged_config {
     int32_t head_dim;          /* 64 or 128 */
     int32_t dtype;             /* CASCADE_F32 or CASCADE_BF16: q, k, v and outputs */
     int32_t page_size;         /* a multiple of 32, at most 65536 */
-    int32_t max_seqs;          /* largest n_seqs of a batch, at most 65536 */
+    int32_t max_seqs;          /* largest n_seqs of a batch, at most 65535 */
     int64_t n_pages;           /* pages in dev_pages */
     float softmax_scale;       /* 0 selects 1/sqrt(head_dim) */
     int32_t window;            /* 0: a query sees every token up to its own; w > 0: the last w of them */

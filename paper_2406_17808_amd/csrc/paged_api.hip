@@ -69,7 +69,7 @@ static int check_paged_config(const cascade_paged_config* c, PagedGeom& g)
     if (c->head_dim != 64 && c->head_dim != 128) return fail(nullptr, CASCADE_E_UNSUPPORTED, "%s: head_dim must be 64 or 128", who);
     if (c->page_size < kGroupTokens || c->page_size > 65536 || c->page_size % kGroupTokens)
         return fail(nullptr, CASCADE_E_INVALID_CONFIG, "%s: page_size must be a multiple of %d, at most 65536", who, kGroupTokens);
-    if (c->max_seqs < 1 || c->max_seqs > 65536) return fail(nullptr, CASCADE_E_INVALID_CONFIG, "%s: max_seqs must be 1 to 65536", who);
+    if (c->max_seqs < 1 || c->max_seqs > 65535) return fail(nullptr, CASCADE_E_INVALID_CONFIG, "%s: max_seqs must be 1 to 65535", who);
     if (!(c->softmax_scale >= 0.f) || !isfinite(c->softmax_scale)) return fail(nullptr, CASCADE_E_INVALID_CONFIG, "%s: softmax_scale must be finite and not negative", who);
     if (c->window < 0) return fail(nullptr, CASCADE_E_INVALID_CONFIG, "%s: window must not be negative", who);
     g.Hq = c->n_q_heads;

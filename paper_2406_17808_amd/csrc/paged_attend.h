@@ -1,0 +1,61 @@
+// Device helpers that the attention kernels of the paged cache share.
+#pragma once
+
+#include "mfma_util.h"
+#include "paged.h"
+
+namespace ckv {
+
+typedef __attribute__((ext_vector_type(4))) float f32x4_t;
+
+constexpr int kFewWaves = 4;        // waves of a workgroup for few rows
+constexpr int kFewRows = 32;        // rows of a sequence and KV head that it takes
+constexpr int kFewParts = 4096;     // most partial results of a launch (sequences x KV heads x splits), of kFewRows rows each
+
+struct FewPlan {
+    int groups_per_split, splits;
+    int max_rows;      // rows of a sequence and KV head: more are left to the other kernel
+};
+
+// Groups of 32 keys that some new token of a sequence sees: [first, last)
+struct KeySpan {
+    int first, last;
+};
+__device__ inline KeySpan key_span(const PagedGeom& g, const PagedBatch& b, const SeqView& v)
+{
+    KeySpan k;
+    const int from = g.window && v.len >= g.window ? v.len - g.window + 1 : 0, to = min(v.len + v.n, b.max_length);
+    k.first = from / kGroupTokens;
+    k.last = max(k.first, (to + kGroupTokens - 1) / kGroupTokens);
+    return k;
+}
+
+// The scale of a K block as the conversion takes it; NaN for byte 255.
+__device__ inline float scale_of_byte(uint32_t byte) { return __uint_as_float(byte == 255u ? 0x7FC00000u : byte << 23); }
+
+// Eight codes -> bf16 times scale (a power of two): exact.
+__device__ inline Frag bf16_of_codes(uint32_t codes, float scale)
+{
+    Frag f;
+    f.u[0] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(codes, scale, 0));
+    f.u[1] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(codes, scale, 1));
+    f.u[2] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(codes, scale, 2));
+    f.u[3] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(codes, scale, 3));
+    return f;
+}
+
+// Two floats as sums of three bf16 terms (8 + 8 + 8 bits): put(term, the two terms packed).
+template <typename F> __device__ inline void split_terms(float a, float b, F put)
+{
+    const uint32_t x = cvt_pk_bf16(a, b);
+    const float a1 = a - __uint_as_float(x << 16), b1 = b - __uint_as_float(x & 0xFFFF0000u);
+    const uint32_t y = cvt_pk_bf16(a1, b1);
+    put(0, x);
+    put(1, y);
+    put(2, cvt_pk_bf16(a1 - __uint_as_float(y << 16), b1 - __uint_as_float(y & 0xFFFF0000u)));
+}
+
+__device__ inline void store4(float* p, float a, float b, float c, float d) { *(float4*)p = make_float4(a, b, c, d); }
+__device__ inline void store4(bf16_t* p, float a, float b, float c, float d) { *(uint2*)p = make_uint2(cvt_pk_bf16(a, b), cvt_pk_bf16(c, d)); }
+
+}  // namespace ckv
