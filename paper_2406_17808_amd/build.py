@@ -10,7 +10,7 @@ CSRC = os.path.join(_HERE, "csrc")
 LIB_PATH = os.path.join(_HERE, "libcascade_kv.so")
 
 SOURCES = ["api.hip", "structure.cpp", "simulate.cpp", "cache_kernels.hip", "attn_simple.hip", "attn_f32.hip", "attn_stream.hip", "score_mfma.hip", "decode.hip", "ceilings.hip",
-           "paged_api.hip", "norm_rope.hip", "paged_rows.hip", "paged_attend.hip"]
+           "paged_api.hip", "norm_rope.hip", "paged_rows.hip", "paged_attend.hip", "paged_chunk.hip"]
 
 # packed fp32 instructions are switched off for every device compilation of this project
 HIPCC_FLAGS = [

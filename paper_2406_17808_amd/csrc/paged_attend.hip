@@ -292,54 +292,6 @@ template <typename T, int D> __global__ __launch_bounds__(256) void merge_few_ke
     store4(out + ((int64_t)(v.first + i) * g.Hq + hk * g.G + h) * D + c, o[0] * r, o[1] * r, o[2] * r, o[3] * r);
 }
 
-// ------------------------------------------------------------------ many rows
-// A wave per query row: 32 keys at a time, two lanes a key for the logits, then a lane per channel (two at D = 128).
-template <typename T, int D> __global__ __launch_bounds__(64) void attend_row_kernel(PagedGeom g, PagedBatch b, int few_rows, const T* __restrict__ q, int64_t q_stride, T* __restrict__ out)
-{
-    __shared__ float qs[D], ps[32];
-    const int lane = threadIdx.x, t = blockIdx.x, h = blockIdx.y, hk = h / g.G;
-    const int s = seq_of_row(b, t);
-    const SeqView v = seq_view(b, s);
-    const int i = t - v.first, p = v.len + i;
-    if (i < 0 || i >= v.n || v.n * g.G <= few_rows) return;
-    for (int c = lane; c < D; c += 64) qs[c] = Elem<T>::load(q + t * q_stride + h * D + c) * g.scale;
-    __syncthreads();
-    float m = -INFINITY, l = 0.f, o[D / 64] = {};
-    const int from = g.window > 0 && p - g.window + 1 > 0 ? p - g.window + 1 : 0;
-    for (int k0 = from & ~31; k0 <= p; k0 += 32) {
-        const int64_t at = paged_group(g, b, s, k0);
-        if (at < 0) continue;
-        const uint8_t* group = g.pages + (at + (int64_t)hk * g.groups) * g.group_bytes;
-        const int r = lane & 31;
-        float x = 0.f;
-        for (int blk = lane >> 5; blk < D / 32; blk += 2) {
-            float part = 0.f;
-            for (int c = 0; c < 32; ++c) part += qs[32 * blk + c] * fp4_value(group[k_code_byte(32 * blk + c, r)] >> (4 * (c & 1)));
-            x += part * k_scale(group[k_exp_byte(D, blk, r)]);
-        }
-        x += __shfl_xor(x, 32);
-        const bool seen = k0 + r >= from && k0 + r <= p && k0 + r < b.max_length;
-        float top = seen ? x : -INFINITY;
-        for (int w = 16; w; w >>= 1) top = fmaxf(top, __shfl_xor(top, w));
-        const float mn = fmaxf(m, top), shrink = mn == -INFINITY ? 1.f : expf(m - mn);
-        const float e = seen ? expf(x - mn) : 0.f;
-        float sum = e;
-        for (int w = 16; w; w >>= 1) sum += __shfl_xor(sum, w);
-        l = l * shrink + sum;
-        m = mn;
-        __syncthreads();
-        if (lane < 32) ps[r] = seen ? e * bf16_to_f32(*(const bf16_t*)(group + v_scale_byte(D, r))) : 0.f;
-        __syncthreads();
-        for (int y = 0; y < D / 64; ++y) {
-            const int c = lane + 64 * y;
-            float acc = o[y] * shrink;
-            for (int k = 0; k < 32; ++k) acc += ps[k] * fp4_value(group[v_code_byte(D, c >> 5, c & 15, k)] >> (4 * ((c >> 4) & 1)));
-            o[y] = acc;
-        }
-    }
-    for (int y = 0; y < D / 64; ++y) Elem<T>::store(out + ((int64_t)t * g.Hq + h) * D + lane + 64 * y, l == 0.f ? 0.f : o[y] / l);
-}
-
 // ------------------------------------------------------------------ launches
 // Splits of a launch for few rows.  A share is a whole number of rounds of the workgroup's waves: at least one, at most 8, and
 // between them what makes about 1024 workgroups (four for each compute unit); more than 8 only where there would be more than kFewParts.
@@ -364,7 +316,8 @@ static FewPlan few_plan(const PagedGeom& g, const PagedBatch& b)
     return p;
 }
 
-size_t paged_scratch_bytes(const PagedGeom& g) { return (size_t)kFewParts * kFewRows * (g.d + 2) * 4; }
+static_assert(kFewParts * kFewRows <= kChunkPartRows, "one scratch for both");
+size_t paged_scratch_bytes(const PagedGeom& g) { return (size_t)kChunkPartRows * (g.d + 2) * 4; }
 
 void launch_paged_attend(const PagedGeom& g, const PagedBatch& b, const void* q, int64_t q_stride, void* out, void* scratch, int dtype, hipStream_t s)
 {
@@ -381,7 +334,7 @@ void launch_paged_attend(const PagedGeom& g, const PagedBatch& b, const void* q,
         if (p.splits > 1)
             hipLaunchKernelGGL((merge_few_kernel<T, D>), dim3(p.max_rows, g.Hkv, b.n_seqs), dim3(256), 0, s, g, b, p, (const float*)scratch, (T*)out);
         if (rows > kFewRows)
-            hipLaunchKernelGGL((attend_row_kernel<T, D>), dim3(b.n_tokens, g.Hq), dim3(64), 0, s, g, b, p.max_rows, (const T*)q, q_stride, (T*)out);
+            launch_attend_chunk(g, b, p.max_rows, q, q_stride, out, scratch, dtype, s);
     });
 }
 

@@ -1,0 +1,363 @@
+// Attention over the paged cache in 4 bits: many query rows per KV head (chunks of prompts), bound by the matrix cores.
+#include <type_traits>
+
+#include "async_copy.h"
+#include "paged_attend.h"
+
+namespace ckv {
+
+// out = softmax(scale Q K^T) V for a block of 32 * NW rows (token, query head of the group) of one sequence and KV head.
+//
+// v_mfma_f32_32x32x16_bf16, S^T = K Q^T (keys are rows, one lane holds half of a query's 64 keys of a tile), O^T = V^T P^T.  The
+// codes of a tile of 64 keys (two groups) are turned into bf16 once per workgroup, on their way from registers to LDS: every
+// value is exact.  K: rows of D channels.  V: rows of 64 keys, in the order that the groups store them and the accumulators of S^T have them
+// (a lane's keys 8s + 4h + b and 16 + 8s + 4h + b are piece 2s + h of a group); a key's V scale multiplies its probability.
+// 16-byte pieces are XOR-swizzled with the row, so that eight lanes that read or write a column of rows meet eight different sets of banks.
+//
+// NW = 8: the two waves of a SIMD work in opposite phase, one on products (a matrix block: P V of tile t, then K Q^T of tile
+// t + 1) while the other takes exponentials and converts codes (a vector block), with a barrier between phases.  Set x in LDS is K of
+// tile x + 1 and V of tile x: what matrix block x reads.  The early waves (0 - 3) run matrix block x in phase 2x and write K in the vector block before
+// it, phase 2x - 1; the late waves (4 - 7) run it in phase 2x + 1 and write V in phase 2x - 2.  Nobody reads set x after phase
+// 2x + 1, and set x + 2 is written from phase 2x + 2 on: two stages do.
+// NW = 4 (fp32: queries and scaled probabilities are sums of three bf16 terms, three times the products and the query registers): all waves are early and convert
+// K and V.
+template <typename T, int D, int NW> __global__ __launch_bounds__(NW * 64, 1) void attend_chunk_kernel(PagedGeom g, PagedBatch b, ChunkPlan plan, const T* __restrict__ q, int64_t q_stride,
+                                                                                                   T* __restrict__ out, float* __restrict__ part)
+{
+    constexpr int kTerms = sizeof(T) == 2 ? 1 : 3, KS = D / 16, DB = D / 32, kRows = 32 * NW;
+    constexpr int kItems = 8 / NW;                     // K and / or V pieces that a thread converts
+    constexpr int kWords = D / 32;                     // words of codes a piece has: 8 * kWords channels of a key, or 8 keys of kWords channels
+    __shared__ __attribute__((aligned(16))) bf16_t k_lds[2][kBN * D], v_lds[2][kBN * D];
+    __shared__ __attribute__((aligned(16))) float vs_lds[2][kBN];
+
+    const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), l = tid & 63, l32 = l & 31, half = l >> 5;
+    const bool late = NW == 8 && wave >= 4;
+    // consecutive workgroups: different KV heads; the blocks of a sequence from its end, which see most keys
+    const int hk = blockIdx.x % g.Hkv, split = blockIdx.y;
+    int s, block;
+    if (!find_row_block(g, b, plan, gridDim.x / g.Hkv - 1 - blockIdx.x / g.Hkv, kRows, s, block)) return;
+    const SeqView v = seq_view(b, s);
+    const int rows = v.n * g.G, row0 = block * kRows;
+
+    // positions that a row sees: [from, to)
+    auto pos_of = [&](int row) { return v.len + min(row, rows - 1) / g.G; };
+    auto from_of = [&](int pos) { return g.window ? max(0, pos - g.window + 1) : 0; };
+    auto to_of = [&](int pos) { return min(pos + 1, b.max_length); };
+    const int row = row0 + wave * 32 + l32, pos = pos_of(row), from = from_of(pos), to = to_of(pos);
+    const int wave_first = pos_of(row0 + wave * 32), wave_last = pos_of(row0 + wave * 32 + 31);
+    const int whole_from = from_of(wave_last), whole_to = to_of(wave_first), any_from = from_of(wave_first), any_to = to_of(wave_last);
+    int tile0 = from_of(pos_of(row0)) / kBN, tile1 = (to_of(pos_of(row0 + kRows - 1)) + kBN - 1) / kBN;
+    tile1 = max(tile1, tile0);
+    if (plan.splits > 1) {
+        const int n = tile1 - tile0;
+        tile1 = tile0 + (int)((int64_t)n * (split + 1) / plan.splits);
+        tile0 += (int)((int64_t)n * split / plan.splits);
+    }
+    const int NT = tile1 - tile0;
+
+    Frag qf[kTerms][KS];
+    {
+        const int r = min(row, rows - 1), i = r / g.G, h = r - i * g.G;
+        const T* x = q + (v.first + i) * q_stride + (hk * g.G + h) * D + 8 * half;
+#pragma unroll
+        for (int ks = 0; ks < KS; ++ks) {
+            if constexpr (kTerms == 1) {
+                qf[0][ks].u = *(const u32x4_t*)(x + 16 * ks);
+            } else {
+                float y[8];
+                *(float4*)y = *(const float4*)(x + 16 * ks);
+                *(float4*)(y + 4) = *(const float4*)(x + 16 * ks + 4);
+#pragma unroll
+                for (int e = 0; e < 8; e += 2) split_terms(y[e], y[e + 1], [&](int term, uint32_t pair) { qf[term][ks].u[e / 2] = pair; });
+            }
+        }
+    }
+    f32x16_t o[DB], st[2];
+#pragma unroll
+    for (int db = 0; db < DB; ++db)
+#pragma unroll
+        for (int j = 0; j < 16; ++j) o[db][j] = 0.f;
+    float top = -INFINITY, sum = 0.f;
+    const float scale = g.scale * 1.44269504088896341f;
+
+    // whether a group is missing anywhere in the range: then every tile looks for itself
+    bool missing = false;
+    for (int i = tid; i < 2 * NT; i += NW * 64) {
+        const int p = (2 * tile0 + i) * kGroupTokens;
+        missing |= p < to_of(pos_of(row0 + kRows - 1)) && paged_group(g, b, s, p) < 0;
+    }
+    missing = __syncthreads_or(missing);
+
+    // ---- codes -> LDS.  Piece kind 0: K, waves 0 - 3 of eight; kind 1: V.  A wave's pieces are of one group of the tile.
+    struct Piece {
+        uint32_t w[kWords];
+        uint32_t extra;      // K: the exponent byte; V: the bits of a scale
+    };
+    // item i of a wave is pieces 64 (w % 2) .. of group w / 2 % 2, w = wave + NW * i; K for w < 4
+    auto load_piece = [&](int item, int tile, Piece& x) {
+        const int w = wave + NW * item, gi = (w & 3) >> 1;      // group of the tile
+        const int64_t at = paged_group(g, b, s, ((tile0 + tile) * 2 + gi) * kGroupTokens);
+        const uint8_t* group = g.pages + ((at < 0 ? 0 : at) + (int64_t)hk * g.groups) * g.group_bytes;
+        const int n = (w & 1) * 64 + l;      // piece of the group, 0 .. 127
+        if (w < 4) {
+            if constexpr (D == 128) {      // block n / 32 of key n % 32
+                const u32x4_t c = *(const u32x4_t*)(group + n * 16);
+                x.w[0] = c[0]; x.w[1] = c[1]; x.w[2] = c[2]; x.w[3] = c[3];
+                x.extra = group[k_exp_byte(D, n >> 5, n & 31)];
+            } else {                       // half n % 2 of block n / 64 of key n / 2 % 32
+                const uint2 c = *(const uint2*)(group + n * 8);
+                x.w[0] = c.x; x.w[1] = c.y;
+                x.extra = group[k_exp_byte(D, n >> 6, (n >> 1) & 31)];
+            }
+        } else {
+            if constexpr (D == 128) {
+                const u32x4_t c = *(const u32x4_t*)(group + 16 * D + n * 16);
+                x.w[0] = c[0]; x.w[1] = c[1]; x.w[2] = c[2]; x.w[3] = c[3];
+            } else {
+                const uint2 c = *(const uint2*)(group + 16 * D + n * 8);
+                x.w[0] = c.x; x.w[1] = c.y;
+            }
+            if ((w & 1) == 0 && l < 32) x.extra = at < 0 ? 0u : (uint32_t)*(const uint16_t*)(group + 33 * D + 2 * l) << 16;
+        }
+    };
+    auto write_piece = [&](int item, int stage, const Piece& x) {
+        const int w = wave + NW * item, gi = (w & 3) >> 1, n = (w & 1) * 64 + l;
+        if (w < 4) {
+            const float ks = scale_of_byte(x.extra);
+            const int r = 32 * gi + (D == 128 ? n & 31 : (n >> 1) & 31);
+            const int piece = D == 128 ? 4 * (n >> 5) : 4 * (n >> 6) + 2 * (n & 1);      // 8 channels each
+#pragma unroll
+            for (int e = 0; e < kWords; ++e) *(u32x4_t*)&k_lds[stage][r * D + ((piece + e) ^ (r & 7)) * 8] = bf16_of_codes(x.w[e], ks).u;
+        } else {
+            // D = 128: chunk n / 64, keys 4q + b, 16 + 4q + b with q = n / 16 % 4, channels n % 16 + 16 (0 .. 3) of 64; D = 64: half of that
+            const int c16 = D == 128 ? n : n >> 1, ch0 = (D == 128 ? 64 * (n >> 6) : 32 * (n & 1)) + (c16 & 15), quarter = (c16 >> 4) & 3;
+#pragma unroll
+            for (int e = 0; e < kWords; e += 2) {
+                const uint32_t a = x.w[e], c = x.w[e + 1];
+                const uint32_t lo = (a & 0x0F0F0F0Fu) | ((c << 4) & 0xF0F0F0F0u), hi = ((a >> 4) & 0x0F0F0F0Fu) | (c & 0xF0F0F0F0u);
+                const int ch = ch0 + 16 * e;
+                *(u32x4_t*)&v_lds[stage][ch * kBN + ((4 * gi + quarter) ^ (ch & 7)) * 8] = bf16_of_codes(lo, 1.f).u;
+                *(u32x4_t*)&v_lds[stage][(ch + 16) * kBN + ((4 * gi + quarter) ^ (ch & 7)) * 8] = bf16_of_codes(hi, 1.f).u;
+            }
+            if ((w & 1) == 0 && l < 32) vs_lds[stage][32 * gi + l] = __uint_as_float(x.extra);
+        }
+    };
+    auto tile_of = [&](int item, int set) { return wave + NW * item < 4 ? set + 1 : set; };
+    Piece held[kItems];
+    auto load_set = [&](int set) {
+#pragma unroll
+        for (int i = 0; i < kItems; ++i) {
+            const int t = tile_of(i, set);
+            if (t >= 0 && t < NT) load_piece(i, t, held[i]);
+        }
+    };
+    auto write_set = [&](int set) {
+#pragma unroll
+        for (int i = 0; i < kItems; ++i) {
+            const int t = tile_of(i, set);
+            if (t >= 0 && t < NT) write_piece(i, set & 1, held[i]);
+        }
+    };
+
+    // ---- blocks
+    auto active = [&](int t) { return (tile0 + t) * kBN < any_to && (tile0 + t + 1) * kBN > any_from; };
+    auto whole = [&](int t) { return (tile0 + t) * kBN >= whole_from && (tile0 + t + 1) * kBN <= whole_to && !missing; };      // all rows of the wave see all keys
+    // SOME: rows may not see every key.  A key's scale may be NaN: it must not reach the rows that do not see the key.
+    auto values_block = [&](int stage, auto some) {
+#pragma unroll
+            for (int gi = 0; gi < 2; ++gi)
+#pragma unroll
+                for (int sx = 0; sx < 2; ++sx) {
+                    const float4 s0 = *(const float4*)&vs_lds[stage][32 * gi + 8 * (2 * sx + half)], s1 = *(const float4*)&vs_lds[stage][32 * gi + 8 * (2 * sx + half) + 4];
+                    const float a[4] = {s0.x, s0.y, s0.z, s0.w}, c[4] = {s1.x, s1.y, s1.z, s1.w};
+                    Frag pf[kTerms];
+#pragma unroll
+                    for (int x = 0; x < 4; ++x) {
+                        float p0 = st[gi][4 * sx + x] * a[x], p1 = st[gi][8 + 4 * sx + x] * c[x];
+                        if (decltype(some)::value) {
+                            p0 = st[gi][4 * sx + x] == 0.f ? 0.f : p0;
+                            p1 = st[gi][8 + 4 * sx + x] == 0.f ? 0.f : p1;
+                        }
+                        if constexpr (kTerms == 1) pf[0].u[x] = cvt_pk_bf16(p0, p1);
+                        else split_terms(p0, p1, [&](int term, uint32_t pair) { pf[term].u[x] = pair; });
+                    }
+#pragma unroll
+                    for (int db = 0; db < DB; ++db) {
+                        const int ch = 32 * db + l32;
+                        Frag vf;
+                        vf.u = *(const u32x4_t*)&v_lds[stage][ch * kBN + ((4 * gi + 2 * sx + half) ^ (ch & 7)) * 8];
+#pragma unroll
+                        for (int y = 0; y < kTerms; ++y) o[db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf.v, pf[y].v, o[db], 0, 0, 0);
+                    }
+                }
+    };
+    auto matrix_block = [&](int t) {
+        const int stage = t & 1;
+        if (t >= 0 && active(t)) {
+            if (whole(t)) values_block(stage, std::false_type());
+            else values_block(stage, std::true_type());
+        }
+        if (t + 1 < NT && active(t + 1)) {
+#pragma unroll
+            for (int kb = 0; kb < 2; ++kb)
+#pragma unroll
+                for (int j = 0; j < 16; ++j) st[kb][j] = 0.f;
+#pragma unroll
+            for (int ks = 0; ks < KS; ++ks)
+#pragma unroll
+                for (int kb = 0; kb < 2; ++kb) {
+                    const int r = 32 * kb + l32;
+                    Frag kf;
+                    kf.u = *(const u32x4_t*)&k_lds[stage][r * D + ((2 * ks + half) ^ (r & 7)) * 8];
+#pragma unroll
+                    for (int y = 0; y < kTerms; ++y) st[kb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf.v, qf[y][ks].v, st[kb], 0, 0, 0);
+                }
+        }
+    };
+    auto softmax = [&](int t) {
+        if (!active(t)) return;
+        const int key0 = (tile0 + t) * kBN;
+        if (!whole(t)) {
+#pragma unroll
+            for (int kb = 0; kb < 2; ++kb) {
+                const bool gone = missing && paged_group(g, b, s, key0 + 32 * kb) < 0;
+#pragma unroll
+                for (int j = 0; j < 16; ++j) {
+                    const int key = key0 + 32 * kb + 8 * (j >> 2) + 4 * half + (j & 3);
+                    if (gone || key < from || key >= to) st[kb][j] = -INFINITY;
+                }
+            }
+        }
+        float mx = -INFINITY;
+#pragma unroll
+        for (int kb = 0; kb < 2; ++kb)
+#pragma unroll
+            for (int j = 0; j < 16; ++j) mx = fmaxf(mx, st[kb][j]);
+        mx *= scale;
+        if (__ballot(mx > top + kRescaleLog2)) {
+            const float now = fmaxf(top, max_xor32(mx));
+            const float shrink = now == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(top - now);
+            top = now;
+            sum *= shrink;
+#pragma unroll
+            for (int db = 0; db < DB; ++db)
+#pragma unroll
+                for (int j = 0; j < 16; ++j) o[db][j] *= shrink;
+        }
+        const float ref = top == -INFINITY ? 0.f : top;      // a row that has seen nothing: every exponential is 0
+#pragma unroll
+        for (int kb = 0; kb < 2; ++kb)
+#pragma unroll
+            for (int j = 0; j < 16; ++j) {
+                st[kb][j] = __builtin_amdgcn_exp2f(__builtin_fmaf(st[kb][j], scale, -ref));
+                sum += st[kb][j];
+            }
+    };
+    auto barrier = [&]() {
+        wait_lds_reads();      // what this wave has written to LDS is there
+        wg_barrier();
+    };
+
+    // ---- the tiles.  A wave converts set t + lead in vector block t + 1.
+    const int lead = late ? 2 : 1;
+    for (int set = -1; set < lead - 1; ++set) {
+        load_set(set);
+        write_set(set);
+    }
+    load_set(lead - 1);
+    barrier();
+    if (late) barrier();
+    for (int t = -1; t < NT; ++t) {
+        matrix_block(t);
+        barrier();
+        if (t + 1 < NT) {
+            write_set(t + lead);
+            load_set(t + lead + 1);
+            softmax(t + 1);
+        }
+        barrier();
+    }
+    if (!late && NW == 8) barrier();
+
+    // ---- rows out: lane l has channels 32 db + 8 (j / 4) + 4 half + j % 4 of its row
+    const auto both = __builtin_amdgcn_permlane32_swap(__float_as_uint(sum), __float_as_uint(sum), false, false);
+    const float total = __uint_as_float(both[0]) + __uint_as_float(both[1]);
+    if (row >= rows) return;
+    if (plan.splits == 1) {
+        const int i = row / g.G, h = row - i * g.G;
+        T* y = out + ((int64_t)(v.first + i) * g.Hq + hk * g.G + h) * D + 4 * half;
+        const float r = total == 0.f ? 0.f : 1.f / total;
+#pragma unroll
+        for (int db = 0; db < DB; ++db)
+#pragma unroll
+            for (int j = 0; j < 16; j += 4) store4(y + 32 * db + 2 * j, o[db][j] * r, o[db][j + 1] * r, o[db][j + 2] * r, o[db][j + 3] * r);
+    } else {
+        const int64_t unit = (int64_t)(gridDim.x / g.Hkv - 1 - blockIdx.x / g.Hkv) * g.Hkv + hk;
+        float* y = part + ((unit * plan.splits + split) * kRows + wave * 32 + l32) * (D + 2);
+#pragma unroll
+        for (int db = 0; db < DB; ++db)
+#pragma unroll
+            for (int j = 0; j < 16; j += 2) *(float2*)(y + 32 * db + 8 * (j >> 2) + 4 * half + (j & 3)) = make_float2(o[db][j], o[db][j + 1]);
+        if (half == 0) *(float2*)(y + D) = make_float2(top, total);
+    }
+}
+
+// Joins the splits: D/4 threads a row, four channels each.
+template <typename T, int D> __global__ __launch_bounds__(256) void merge_chunk_kernel(PagedGeom g, PagedBatch b, ChunkPlan plan, int block_rows, const float* __restrict__ part, T* __restrict__ out)
+{
+    constexpr int kLanes = D / 4, kRowsHere = 256 / kLanes;
+    const int unit = blockIdx.x, hk = blockIdx.y;
+    int s, block;
+    if (!find_row_block(g, b, plan, unit, block_rows, s, block)) return;
+    const SeqView v = seq_view(b, s);
+    const int in_block = blockIdx.z * kRowsHere + threadIdx.x / kLanes, row = block * block_rows + in_block, c = threadIdx.x % kLanes * 4;
+    if (row >= v.n * g.G) return;
+    const float* x = part + ((int64_t)(unit * g.Hkv + hk) * plan.splits * block_rows + in_block) * (D + 2);
+    const int64_t step = (int64_t)block_rows * (D + 2);
+    float top = -INFINITY;
+    for (int i = 0; i < plan.splits; ++i) top = fmaxf(top, x[i * step + D]);
+    float l = 0.f, o[4] = {};
+    for (int i = 0; i < plan.splits; ++i) {
+        const float m = x[i * step + D], f = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m - top);
+        const float2 a = *(const float2*)(x + i * step + c), e = *(const float2*)(x + i * step + c + 2);
+        l += f * x[i * step + D + 1];
+        o[0] += f * a.x;
+        o[1] += f * a.y;
+        o[2] += f * e.x;
+        o[3] += f * e.y;
+    }
+    const int i = row / g.G, h = row - i * g.G;
+    const float r = l == 0.f ? 0.f : 1.f / l;
+    store4(out + ((int64_t)(v.first + i) * g.Hq + hk * g.G + h) * D + c, o[0] * r, o[1] * r, o[2] * r, o[3] * r);
+}
+
+// Splits of a launch that has fewer row blocks than compute units: as many workgroups as there are of those, eight tiles each at least.
+ChunkPlan chunk_plan(const PagedGeom& g, const PagedBatch& b, int few_rows, int block_rows)
+{
+    ChunkPlan p;
+    p.few_rows = few_rows;
+    // a sequence's last block may be short
+    p.units = (int)(((int64_t)b.n_tokens * g.G + block_rows - 1) / block_rows) + b.n_seqs;
+    const int64_t longest = g.window && g.window < b.max_length - b.max_new ? g.window + b.max_new + kBN : b.max_length;
+    const int64_t tiles = longest / kBN + 1, pairs = (int64_t)(p.units - b.n_seqs + (b.n_seqs + 1) / 2) * g.Hkv;
+    int64_t n = 256 / pairs;
+    if (n > tiles / 8) n = tiles / 8;
+    const int64_t most = (int64_t)kChunkPartRows / ((int64_t)p.units * g.Hkv * block_rows);
+    if (n > most) n = most;
+    p.splits = n < 1 ? 1 : (int)n;
+    return p;
+}
+
+void launch_attend_chunk(const PagedGeom& g, const PagedBatch& b, int few_rows, const void* q, int64_t q_stride, void* out, void* scratch, int dtype, hipStream_t s)
+{
+    with_paged_form(dtype, g.d, [&](auto f) {
+        typedef typename decltype(f)::Elt T;
+        constexpr int D = decltype(f)::d, NW = sizeof(T) == 2 ? 8 : 4;
+        const ChunkPlan p = chunk_plan(g, b, few_rows, 32 * NW);
+        hipLaunchKernelGGL((attend_chunk_kernel<T, D, NW>), dim3(p.units * g.Hkv, p.splits), dim3(NW * 64), 0, s, g, b, p, (const T*)q, q_stride, (T*)out, (float*)scratch);
+        if (p.splits > 1)
+            hipLaunchKernelGGL((merge_chunk_kernel<T, D>), dim3(p.units, g.Hkv, 32 * NW * D / 1024), dim3(256), 0, s, g, b, p, 32 * NW, (const float*)scratch, (T*)out);
+    });
+}
+
+}  // namespace ckv
