@@ -1,6 +1,5 @@
 // The rotation table, and the RMS norm of queries and keys per head with the rotation in the same pass.
-#include "mfma_util.h"
-#include "paged.h"
+#include "row_pieces.h"
 
 namespace ckv {
 
@@ -80,12 +79,100 @@ template <typename T> __global__ __launch_bounds__(256) void norm_rope_any_kerne
     }
 }
 
+// Rows of whole 16-byte pieces, TPR threads a row (the first d / 16 of them work), each with 8 channels of the lower half and their partners of
+// the upper half: the rotation needs no exchange.  A workgroup has all rows of `per` tokens (or, with more than 1024 / TPR rows a token, goes over
+// them), whose cosines and sines are made once, in LDS, while the rows are on their way.
+template <typename T, int TPR> __global__ __launch_bounds__(1024) void norm_rope_kernel(NormRope a, int per)
+{
+    extern __shared__ float2 cs[];      // [per][d / 2]
+    const int half = a.d / 2, heads = a.Hq + a.Hk, t0 = blockIdx.x * per, tokens = min(per, a.n_tokens - t0);
+    const int j = threadIdx.x % TPR, work = tokens * heads;
+    const bool on = j < a.d / 16;
+    int row = threadIdx.x / TPR;
+    float lo[8], hi[8];
+    const T* w = nullptr;
+    T* y = nullptr;
+    int t = 0;
+    auto load = [&]() {
+        t = row / heads;
+        const int h = row - t * heads;
+        const bool is_q = h < a.Hq;
+        const int64_t at = t0 + t;
+        const T* x = is_q ? (const T*)a.q + at * a.q_stride + h * a.d : (const T*)a.k + at * a.k_stride + (h - a.Hq) * a.d;
+        y = is_q ? (T*)a.q_out + at * a.q_out_stride + h * a.d : (T*)a.k_out + at * a.k_out_stride + (h - a.Hq) * a.d;
+        w = (const T*)(is_q ? a.q_weight : a.k_weight);
+        load8(x + 8 * j, lo);
+        load8(x + half + 8 * j, hi);
+    };
+    if (row < work && on) load();
+    if (a.positions) {
+        for (int i = threadIdx.x; i < tokens * half; i += blockDim.x) cs[i] = cos_sin(a, t0 + i / half, i % half);
+        __syncthreads();
+    }
+    while (row < work) {
+        if (a.norm) {
+            float sum = 0.f;
+            if (on)
+#pragma unroll
+                for (int e = 0; e < 8; ++e) sum += lo[e] * lo[e] + hi[e] * hi[e];
+#pragma unroll
+            for (int o = 1; o < TPR; o <<= 1) sum += __shfl_xor(sum, o);
+            const float r = 1.f / sqrtf(sum / (float)a.d + a.eps);
+            float wl[8], wh[8];
+            if (w && on) {
+                load8(w + 8 * j, wl);
+                load8(w + half + 8 * j, wh);
+            }
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                lo[e] *= w ? r * wl[e] : r;
+                hi[e] *= w ? r * wh[e] : r;
+            }
+        }
+        if (on) {
+            if (a.positions)
+#pragma unroll
+                for (int e = 0; e < 8; ++e) {
+                    const float2 c = cs[t * half + 8 * j + e];
+                    const float x = lo[e], z = hi[e];
+                    lo[e] = rot_lo(x, z, c.x, c.y);
+                    hi[e] = rot_hi(x, z, c.x, c.y);
+                }
+            store8(y + 8 * j, lo);
+            store8(y + half + 8 * j, hi);
+        }
+        row += blockDim.x / TPR;
+        if (row < work && on) load();
+    }
+}
+
+template <typename T> static void launch_norm_rope_typed(const NormRope& a, hipStream_t s)
+{
+    const int heads = a.Hq + a.Hk;
+    if (!a.vectors) {
+        const int64_t blocks = ((int64_t)a.n_tokens * heads + 3) / 4;
+        hipLaunchKernelGGL((norm_rope_any_kernel<T>), dim3((unsigned)(blocks < 65536 ? blocks : 65536)), dim3(256), 0, s, a);
+        return;
+    }
+    int tpr = 1;
+    while (tpr < a.d / 16) tpr *= 2;
+    // as many tokens as make 256 threads; a token with more than 1024 threads' rows is gone over in rounds
+    const int each = heads * tpr, per = each >= 256 ? 1 : 256 / each, threads = (each * per + 63) / 64 * 64;
+    const dim3 grid((a.n_tokens + per - 1) / per), block(threads > 1024 ? 1024 : threads);
+    const size_t lds = (size_t)per * (a.d / 2) * sizeof(float2);
+    switch (tpr) {
+    case 1: hipLaunchKernelGGL((norm_rope_kernel<T, 1>), grid, block, lds, s, a, per); break;
+    case 2: hipLaunchKernelGGL((norm_rope_kernel<T, 2>), grid, block, lds, s, a, per); break;
+    case 4: hipLaunchKernelGGL((norm_rope_kernel<T, 4>), grid, block, lds, s, a, per); break;
+    case 8: hipLaunchKernelGGL((norm_rope_kernel<T, 8>), grid, block, lds, s, a, per); break;
+    default: hipLaunchKernelGGL((norm_rope_kernel<T, 16>), grid, block, lds, s, a, per); break;
+    }
+}
+
 void launch_norm_rope(const NormRope& a, int dtype, hipStream_t s)
 {
-    const int64_t rows = (int64_t)a.n_tokens * (a.Hq + a.Hk);
-    const dim3 grid((unsigned)(rows / 4 + 1 < 65536 ? rows / 4 + 1 : 65536));
-    if (dtype == CASCADE_BF16) hipLaunchKernelGGL((norm_rope_any_kernel<bf16_t>), grid, dim3(256), 0, s, a);
-    else hipLaunchKernelGGL((norm_rope_any_kernel<float>), grid, dim3(256), 0, s, a);
+    if (dtype == CASCADE_BF16) launch_norm_rope_typed<bf16_t>(a, s);
+    else launch_norm_rope_typed<float>(a, s);
 }
 
 }  // namespace ckv

@@ -14,19 +14,25 @@ from . import binding as B
 _TYPES = {torch.bfloat16: B.CASCADE_BF16, torch.float32: B.CASCADE_F32}
 
 
+# The current stream as a number, without the stream object around it (0.1 instead of 2 us of a call's host time).
+_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+
+
 def _stream(device: torch.device) -> int:
+    if _raw_stream is not None and device.index is not None:
+        return _raw_stream(device.index)
     return torch.cuda.current_stream(device).cuda_stream
 
 
-def _check_rows(x: torch.Tensor, device, dtype, heads: int, head_dim: int, tokens: Optional[int] = None) -> None:
-    """[tokens, heads, head_dim] with the heads of a token next to each other; tokens may lie further apart."""
-    assert x.is_cuda and x.device == device and x.dtype == dtype and x.dim() == 3, (x.device, x.dtype, tuple(x.shape))
-    assert x.shape[1:] == (heads, head_dim) and (tokens is None or x.shape[0] == tokens), (tuple(x.shape), tokens, heads, head_dim)
-    assert x.numel() == 0 or ((x.stride(2) == 1 or head_dim == 1) and (x.stride(1) == head_dim or heads == 1)), x.stride()
-
-
-def _row_stride(x: torch.Tensor) -> int:
-    return x.stride(0) if x.shape[0] > 1 else 0      # the stride of a single token says nothing
+def _rows(x: torch.Tensor, device, dtype, tokens: int, heads: int, head_dim: int) -> int:
+    """Checks [tokens, heads, head_dim] with the heads of a token next to each other; returns how far apart the tokens lie (0: next to each other)."""
+    strides = x.stride()
+    if x.dtype is not dtype or x.device != device or x.shape != (tokens, heads, head_dim) or strides[1:] != (head_dim, 1):
+        # strides of dimensions of one element say nothing
+        fits = x.dtype is dtype and x.device == device and x.shape == (tokens, heads, head_dim)
+        assert fits and ((strides[2] == 1 or head_dim == 1) and (strides[1] == head_dim or heads == 1) or x.numel() == 0), \
+            (x.device, x.dtype, tuple(x.shape), strides, "wanted", device, dtype, (tokens, heads, head_dim))
+    return strides[0] if tokens > 1 else 0
 
 
 class RopeTable:
@@ -49,33 +55,32 @@ def qk_norm_rope(q: torch.Tensor, k: Optional[torch.Tensor] = None, q_weight: Op
     [tokens] (int32; None: not rotated, as CascadeKVCache takes them) in the same pass.  norm=False rotates only.  Tokens
     of q and k may lie apart (views of a fused projection).  q_out / k_out may be q / k."""
     device, dtype, (tokens, hq, d) = q.device, q.dtype, q.shape
-    assert dtype in _TYPES, dtype
-    _check_rows(q, device, dtype, hq, d)
-    a = B.cascade_norm_rope_args(dtype=_TYPES[dtype], head_dim=d, n_tokens=tokens, n_q_heads=hq, norm=int(norm), eps=eps)
+    assert q.is_cuda and dtype in _TYPES, (device, dtype)
     if q_out is None:
         q_out = torch.empty((tokens, hq, d), dtype=dtype, device=device)
-    _check_rows(q_out, device, dtype, hq, d, tokens)
-    a.dev_q, a.dev_q_out, a.q_stride, a.q_out_stride = q.data_ptr(), q_out.data_ptr(), _row_stride(q), _row_stride(q_out)
+    q_stride, q_out_stride = _rows(q, device, dtype, tokens, hq, d), _rows(q_out, device, dtype, tokens, hq, d)
+    hk = k_stride = k_out_stride = 0
     if k is not None:
         hk = k.shape[1]
-        _check_rows(k, device, dtype, hk, d, tokens)
         if k_out is None:
             k_out = torch.empty((tokens, hk, d), dtype=dtype, device=device)
-        _check_rows(k_out, device, dtype, hk, d, tokens)
-        a.n_k_heads = hk
-        a.dev_k, a.dev_k_out, a.k_stride, a.k_out_stride = k.data_ptr(), k_out.data_ptr(), _row_stride(k), _row_stride(k_out)
+        k_stride, k_out_stride = _rows(k, device, dtype, tokens, hk, d), _rows(k_out, device, dtype, tokens, hk, d)
     else:
         assert k_out is None and k_weight is None
     for w in (q_weight, k_weight):
-        assert w is None or (norm and w.device == device and w.dtype == dtype and tuple(w.shape) == (d,) and w.is_contiguous())
-    a.dev_q_weight = q_weight.data_ptr() if q_weight is not None else None
-    a.dev_k_weight = k_weight.data_ptr() if k_weight is not None else None
+        assert w is None or (norm and w.device == device and w.dtype == dtype and w.shape == (d,) and w.is_contiguous())
     if positions is not None:
-        assert positions.device == device and positions.dtype == torch.int32 and tuple(positions.shape) == (tokens,) and positions.is_contiguous()
+        assert positions.device == device and positions.dtype == torch.int32 and positions.shape == (tokens,) and positions.is_contiguous()
         assert rope is not None and rope.device == device and rope.head_dim == d, "positions need a RopeTable of this head_dim"
-        a.dev_positions, a.dev_rope, a.rope_positions = positions.data_ptr(), rope.table.data_ptr(), rope.n_positions
-    with torch.cuda.device(device):
-        B.cascade_norm_rope(a, _stream(device))
+    args = B.cascade_norm_rope_args(
+        _TYPES[dtype], d, tokens, hq, hk, norm, eps, 0, q.data_ptr(), k.data_ptr() if hk else None, q_out.data_ptr(), k_out.data_ptr() if hk else None,
+        q_stride, k_stride, q_out_stride, k_out_stride, None if q_weight is None else q_weight.data_ptr(), None if k_weight is None else k_weight.data_ptr(),
+        *((None, None, 0) if positions is None else (positions.data_ptr(), rope.table.data_ptr(), rope.n_positions)))
+    if torch.cuda.current_device() == device.index:
+        B.cascade_norm_rope(args, _stream(device))
+    else:
+        with torch.cuda.device(device):
+            B.cascade_norm_rope(args, _stream(device))
     return q_out, k_out
 
 
@@ -90,6 +95,7 @@ class PagedBatch:
             assert x.is_cuda and x.dtype == torch.int32 and x.device == lengths.device, (x.device, x.dtype)
         assert lengths.dim() == 1 and lengths.is_contiguous() and tuple(new_offsets.shape) == (n + 1,) and new_offsets.is_contiguous()
         assert page_table.dim() == 2 and page_table.shape[0] == n and page_table.is_contiguous()
+        self.device = lengths.device
         self.lengths, self.new_offsets, self.page_table = lengths, new_offsets, page_table
         self.n_tokens, self.max_new, self.max_length = int(n_tokens), int(max_new), int(max_length)
         self.c = B.cascade_paged_batch(n_seqs=n, n_tokens=self.n_tokens, max_new=self.max_new, max_length=self.max_length,
@@ -103,6 +109,7 @@ class PagedKVCache:
 
     def __init__(self, cfg: B.cascade_paged_config, device: str = "cuda:0", pages: Optional[torch.Tensor] = None, rope: Optional[RopeTable] = None):
         self.cfg, self.rope = cfg, rope
+        self.n_q_heads, self.n_kv_heads, self.head_dim = cfg.n_q_heads, cfg.n_kv_heads, cfg.head_dim
         self.device = torch.device(device)
         self.torch_dtype = torch.bfloat16 if cfg.dtype == B.CASCADE_BF16 else torch.float32
         self.page_bytes = B.cascade_paged_page_bytes(cfg)
@@ -134,39 +141,38 @@ class PagedKVCache:
     def append(self, batch: PagedBatch, k: torch.Tensor, v: torch.Tensor, q: Optional[torch.Tensor] = None,
                q_out: Optional[torch.Tensor] = None) -> Optional[torch.Tensor]:
         """Stores k, v [n_tokens, kv heads, head_dim] of the batch's new tokens; q [n_tokens, q heads, head_dim] is rotated into q_out, which is returned."""
-        c = self.cfg
-        assert batch.lengths.device == self.device
-        _check_rows(k, self.device, self.torch_dtype, c.n_kv_heads, c.head_dim, batch.n_tokens)
-        _check_rows(v, self.device, self.torch_dtype, c.n_kv_heads, c.head_dim, batch.n_tokens)
-        if q is not None:
-            _check_rows(q, self.device, self.torch_dtype, c.n_q_heads, c.head_dim, batch.n_tokens)
-            if q_out is None:
-                q_out = torch.empty((batch.n_tokens, c.n_q_heads, c.head_dim), dtype=self.torch_dtype, device=self.device)
-            _check_rows(q_out, self.device, self.torch_dtype, c.n_q_heads, c.head_dim, batch.n_tokens)
-            assert q_out.is_contiguous()
-        else:
+        n, d, device, dtype = batch.n_tokens, self.head_dim, self.device, self.torch_dtype
+        assert batch.device == device
+        k_stride, v_stride = _rows(k, device, dtype, n, self.n_kv_heads, d), _rows(v, device, dtype, n, self.n_kv_heads, d)
+        if q is None:
             assert q_out is None
-        B.cascade_paged_append(self.ctx, batch.c, k.data_ptr(), _row_stride(k), v.data_ptr(), _row_stride(v),
-                               q.data_ptr() if q is not None else 0, _row_stride(q) if q is not None else 0,
-                               q_out.data_ptr() if q is not None else 0, _stream(self.device))
+            B.cascade_paged_append(self.ctx, batch.c, k.data_ptr(), k_stride, v.data_ptr(), v_stride, 0, 0, 0, _stream(device))
+            return None
+        q_stride = _rows(q, device, dtype, n, self.n_q_heads, d)
+        if q_out is None:
+            q_out = torch.empty((n, self.n_q_heads, d), dtype=dtype, device=device)
+        else:
+            _rows(q_out, device, dtype, n, self.n_q_heads, d)
+            assert q_out.is_contiguous()
+        B.cascade_paged_append(self.ctx, batch.c, k.data_ptr(), k_stride, v.data_ptr(), v_stride, q.data_ptr(), q_stride, q_out.data_ptr(), _stream(device))
         return q_out
 
     def attend(self, batch: PagedBatch, q: torch.Tensor, out: Optional[torch.Tensor] = None) -> torch.Tensor:
         """Attention of q [n_tokens, q heads, head_dim], rotated, over the cache, the batch's new tokens included."""
-        c = self.cfg
-        assert batch.lengths.device == self.device
-        _check_rows(q, self.device, self.torch_dtype, c.n_q_heads, c.head_dim, batch.n_tokens)
+        n, d, device, dtype = batch.n_tokens, self.head_dim, self.device, self.torch_dtype
+        assert batch.device == device
+        q_stride = _rows(q, device, dtype, n, self.n_q_heads, d)
         if out is None:
-            out = torch.empty((batch.n_tokens, c.n_q_heads, c.head_dim), dtype=self.torch_dtype, device=self.device)
-        _check_rows(out, self.device, self.torch_dtype, c.n_q_heads, c.head_dim, batch.n_tokens)
-        assert out.is_contiguous()
-        B.cascade_paged_attend(self.ctx, batch.c, q.data_ptr(), _row_stride(q), out.data_ptr(), _stream(self.device))
+            out = torch.empty((n, self.n_q_heads, d), dtype=dtype, device=device)
+        else:
+            _rows(out, device, dtype, n, self.n_q_heads, d)
+            assert out.is_contiguous()
+        B.cascade_paged_attend(self.ctx, batch.c, q.data_ptr(), q_stride, out.data_ptr(), _stream(device))
         return out
 
     def read(self, batch: PagedBatch) -> Tuple[torch.Tensor, torch.Tensor]:
         """The rows that the batch calls new, as the values their codes stand for."""
-        c = self.cfg
-        assert batch.lengths.device == self.device
-        k, v = (torch.empty((batch.n_tokens, c.n_kv_heads, c.head_dim), dtype=self.torch_dtype, device=self.device) for _ in range(2))
+        assert batch.device == self.device
+        k, v = (torch.empty((batch.n_tokens, self.n_kv_heads, self.head_dim), dtype=self.torch_dtype, device=self.device) for _ in range(2))
         B.cascade_paged_read(self.ctx, batch.c, k.data_ptr(), v.data_ptr(), _stream(self.device))
         return k, v
