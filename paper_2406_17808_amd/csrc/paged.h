@@ -30,6 +30,36 @@ __device__ inline int seq_of_row(const PagedBatch& b, int t)
     return __builtin_amdgcn_readfirstlane(lo);
 }
 
+// Unit `unit` of a batch whose sequences have count(SeqView) units each: its sequence and its number there; false behind the last.  Called by whole
+// waves, unit the same in all lanes.
+template <typename F> __device__ inline bool find_unit(const PagedBatch& b, F count, int unit, int& seq, int& number)
+{
+    const int l = threadIdx.x & 63;
+    if (b.n_seqs == 1) {
+        seq = 0;
+        number = unit;
+        return unit < count(seq_view(b, 0));
+    }
+    for (int s0 = 0; s0 < b.n_seqs; s0 += 64) {
+        const int n = s0 + l < b.n_seqs ? count(seq_view(b, s0 + l)) : 0;
+        int upto = n;      // units of the sequences up to this lane's
+#pragma unroll
+        for (int o = 1; o < 64; o <<= 1) {
+            const int x = __shfl_up(upto, o);
+            if (l >= o) upto += x;
+        }
+        const int all = __builtin_amdgcn_readlane(upto, 63);
+        if (unit < all) {
+            const int at = __builtin_popcountll(__ballot(upto <= unit));
+            seq = s0 + at;
+            number = unit - __builtin_amdgcn_readlane(upto - n, at);
+            return true;
+        }
+        unit -= all;
+    }
+    return false;
+}
+
 // ------------------------------------------------------------------ launchers
 // f(PagedForm<element type, head size>{}) for the context's.
 template <typename T, int D> struct PagedForm {

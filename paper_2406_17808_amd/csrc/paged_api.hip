@@ -246,6 +246,11 @@ static int check_batch(cascade_paged_ctx* ctx, const char* who, const cascade_pa
     b.table = x->dev_page_table;
     b.table_stride = x->table_stride;
     if (b.n_seqs == 0 || b.max_new == 0) return CASCADE_OK;
+    // workgroups of up to 512 threads, and 2^32 threads at most in a launch: one per KV head and group of 32 tokens (two of a sequence may be begun) and one per
+    // token (append), or one per KV head and block of 128 rows (one of a sequence may be begun)
+    const int64_t n_groups = b.n_tokens / kGroupTokens + 2 * (int64_t)b.n_seqs;
+    if (n_groups * ctx->g.Hkv + b.n_tokens > (1 << 22) || (int64_t)b.n_tokens * ctx->g.Hq / 128 + (int64_t)b.n_seqs * ctx->g.Hkv > (1 << 22))
+        return fail(ctx, CASCADE_E_BAD_ARG, "%s: too many tokens or sequences for one call", who);
     if (!b.lengths || !b.offsets || (!b.table && b.table_stride)) return fail(ctx, CASCADE_E_NULL_ARG, "%s: NULL array in the batch", who);
     if (!aligned(b.lengths, 4) || !aligned(b.offsets, 4) || !aligned(b.table, 4)) return fail(ctx, CASCADE_E_BAD_ARG, "%s: the batch's arrays must be 4-byte aligned", who);
     n = b.n_tokens;

@@ -27,33 +27,13 @@ struct ChunkPlan {
 ChunkPlan chunk_plan(const PagedGeom& g, const PagedBatch& b, int few_rows, int block_rows);
 void launch_attend_chunk(const PagedGeom& g, const PagedBatch& b, int few_rows, const void* q, int64_t q_stride, void* out, void* scratch, int dtype, hipStream_t s);
 
-// Row block `unit` of a batch, counted over its sequences: the sequence and the block in it; false behind the last.  Called by whole workgroups,
-// unit the same in all lanes.
+// Row block `unit` of a batch, counted over the sequences that have more rows than the other kernel takes.
 __device__ inline bool find_row_block(const PagedGeom& g, const PagedBatch& b, const ChunkPlan& plan, int unit, int block_rows, int& seq, int& block)
 {
-    const int l = threadIdx.x & 63;
-    for (int s0 = 0; s0 < b.n_seqs; s0 += 64) {
-        int n = 0;
-        if (s0 + l < b.n_seqs) {
-            const int rows = seq_view(b, s0 + l).n * g.G;
-            n = rows > plan.few_rows ? (rows + block_rows - 1) / block_rows : 0;
-        }
-        int upto = n;      // row blocks of the sequences up to this lane's
-#pragma unroll
-        for (int o = 1; o < 64; o <<= 1) {
-            const int x = __shfl_up(upto, o);
-            if (l >= o) upto += x;
-        }
-        const int all = __builtin_amdgcn_readlane(upto, 63);
-        if (unit < all) {
-            const int at = __builtin_popcountll(__ballot(upto <= unit));
-            seq = s0 + at;
-            block = unit - __builtin_amdgcn_readlane(upto - n, at);
-            return true;
-        }
-        unit -= all;
-    }
-    return false;
+    return find_unit(b, [&](const SeqView& v) {
+        const int rows = v.n * g.G;
+        return rows > plan.few_rows ? (rows + block_rows - 1) / block_rows : 0;
+    }, unit, seq, block);
 }
 
 // Groups of 32 keys that some new token of a sequence sees: [first, last)

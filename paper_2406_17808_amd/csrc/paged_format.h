@@ -103,24 +103,32 @@ template <typename F> __host__ __device__ inline uint32_t fp4_code(F y, F unit)
     return code | (y < (F)0 ? 8u : 0u);
 }
 
-// Byte of the smallest scale 2^e with top <= 7 * 2^e; 0 for zeros, 255 where top is an infinity or NaN.  top in 64 bits: whether a
-// block takes the next scale is decided by the exact amount.
-__host__ __device__ inline uint32_t k_exponent(double top)
+// |y| of a 64-bit number in 32 bits, for comparisons with numbers of at most 19 mantissa bits: the upper word, with the last bit set where the lower word
+// is not zero.  Which side of such a number y lies on is kept.
+__host__ __device__ inline uint32_t k_key(double y)
 {
     union { double d; uint64_t u; } c;
-    c.d = top;
-    const int biased = (int)(c.u >> 52) & 0x7FF;
+    c.d = y;
+    return ((uint32_t)(c.u >> 32) & 0x7FFFFFFFu) | ((uint32_t)c.u != 0u ? 1u : 0u);
+}
+
+// Byte of the smallest scale 2^e with top <= 7 * 2^e, top the largest key of a block; 0 for zeros, 255 where it is an infinity or NaN.
+__host__ __device__ inline uint32_t k_exponent_of_key(uint32_t top)
+{
+    const int biased = (int)(top >> 20);
     if (biased == 0x7FF) return 255u;
     if (biased < 1023 - 400) return 0u;      // zero, or far below the smallest scale
-    int e = biased - 1023 - 2 + ((c.u & 0xFFFFFFFFFFFFFull) > 0xC000000000000ull ? 1 : 0);      // top = 1.m * 2^(biased - 1023); 1.75 * 4 = 7
+    int e = biased - 1023 - 2 + ((top & 0xFFFFFu) > 0xC0000u ? 1 : 0);      // 1.m * 2^(biased - 1023); 1.75 * 4 = 7
     e = e < -126 ? -126 : e > 127 ? 127 : e;
     return (uint32_t)(e + 127);
 }
-__host__ __device__ inline double pow2_f64(int e)
+__host__ __device__ inline uint32_t k_exponent(double top) { return k_exponent_of_key(k_key(top)); }
+
+// The bits of a float next to |y| / scale of `byte`, on the same side of every number with few bits: rounding it to a code rounds y.  0 for the byte 255.
+__host__ __device__ inline uint32_t k_scaled_bits(uint32_t key, uint32_t byte)
 {
-    union { double d; uint64_t u; } c;
-    c.u = (uint64_t)(e + 1023) << 52;
-    return c.d;
+    const int d = (int)key - ((1023 - 127 + (int)byte - 127) << 20);      // exponents: of y / 2^(byte - 127), with a float's bias
+    return byte == 255u || d < 0 ? 0u : (uint32_t)d << 3;
 }
 
 // Scale of a V row (bf16 bits): top / 6; 0 below 2^-100.  A NaN or infinity in the row gives NaN.

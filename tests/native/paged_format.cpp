@@ -117,7 +117,15 @@ static void numbers()
     CHECK(k_exponent(0.0) == 0 && k_exponent(INFINITY) == 255 && k_exponent(NAN) == 255 && k_exponent(1e-60) == 1 && k_exponent(3.4e38) == 127 + 126);
     CHECK(k_scale(0) == 0.f && k_scale(127) == 1.f && k_scale(1) == ldexpf(1, -126) && isnan(k_scale(255)));
     CHECK(v_scale_bits(0.f) == 0 && v_scale_bits(6.f) == 0x3F80 && v_scale_bits(INFINITY) == 0x7FC0 && v_scale_bits(NAN) == 0x7FC0 && v_scale_bits(1e-35f) == 0);
-    CHECK(pow2_f64(0) == 1.0 && pow2_f64(-127) == ldexp(1, -127) && pow2_f64(127) == ldexp(1, 127));
+    // what the kernels round to a code: a float on the same side of every border as the 64-bit number
+    for (int i = 0; i < 200000; ++i) {
+        const int e = (int)(rng() % 253) - 126;
+        const double border = rint(ldexp((double)(rng() >> 1), -63) * 28) / 4;
+        const double y = i % 4 == 0 ? border : i % 4 == 1 ? nextafter(border, 9) : i % 4 == 2 ? nextafter(border, -1) : ldexp((double)(rng() >> 1), -63) * 7;
+        const uint32_t bits = k_scaled_bits(k_key(ldexp(y, e)), (uint32_t)(e + 127));
+        CHECK(y < 0 || fp4_code((double)f32_from_bits(bits), 1.0) == fp4_code(y, 1.0));
+    }
+    CHECK(k_scaled_bits(k_key(INFINITY), 255) == 0 && k_scaled_bits(k_key(0.0), 0) == 0 && k_scaled_bits(k_key(1e-300), 200) == 0);
 }
 
 int main()
