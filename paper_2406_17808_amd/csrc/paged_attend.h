@@ -12,6 +12,8 @@ constexpr int kFewWaves = 4;        // waves of a workgroup for few rows
 constexpr int kFewRows = 32;        // rows of a sequence and KV head that it takes
 constexpr int kFewParts = 4096;     // most partial results of a launch (sequences x KV heads x splits), of kFewRows rows each
 
+constexpr int kFewMaxSplits = 512;
+
 struct FewPlan {
     int groups_per_split, splits;
     int max_rows;      // rows of a sequence and KV head: more are left to the other kernel

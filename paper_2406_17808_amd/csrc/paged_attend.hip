@@ -1,5 +1,5 @@
 // Attention over the paged cache in 4 bits: a few query rows per KV head (single tokens, a few of them) against a long cache.
-#include "mfma_util.h"
+#include "async_copy.h"
 #include "paged_attend.h"
 
 namespace ckv {
@@ -14,9 +14,10 @@ namespace ckv {
 // go in unscaled; a key's scale is a factor of its probability.  fp32: the queries and the scaled probabilities are sums of three bf16 terms
 // (24 bits), with a product each.
 //
-// A workgroup has kFewWaves waves; wave w takes groups w, w + kFewWaves, ... of the workgroup's share, with the next group's codes on their way
-// while one is worked on.  The running maximum is raised only when a logit exceeds it by 2^8 (in 32 bits
-// nothing is lost below 2^127): a vote instead of an exchange between lanes for most groups.
+// A workgroup has kFewWaves waves; wave w takes groups w, w + kFewWaves, ... of the workgroup's share.  A wave has kFewStages groups of its own in
+// LDS, filled by asynchronous copies (a group is contiguous), and waits only for its own: two workgroups on a compute unit have 120 KB on their way
+// whatever the waves compute.  (Loads to registers, one group ahead, three waves a SIMD: 50 KB, 4.3 TB/s.)  The running maximum is raised only
+// when a logit exceeds it by 2^8 (in 32 bits nothing is lost below 2^127): a vote instead of an exchange between lanes for most groups.
 template <int D> struct GroupCodes {
     u32x4_t k[2];            // D = 64: the first two words
     u32x4_t v[D / 64];
@@ -24,7 +25,19 @@ template <int D> struct GroupCodes {
     uint32_t exps;           // K bytes of keys m and 16 + m
 };
 
-template <int D> __device__ inline void load_group(GroupCodes<D>& c, const uint8_t* __restrict__ group, int m, int q)
+constexpr int kFewStages = 4;
+template <int D> constexpr int few_stage_bytes() { return 32 * D + 256; }      // the codes, and 256 bytes from the scales on
+template <int D> constexpr int few_copies() { return D / 32 + 1; }             // copies of 1 KB, and one of 256 bytes
+
+// One group, to LDS.  The last copy's lanes behind the group (D = 64) read its last word again.
+template <int D> __device__ inline void copy_group(const uint8_t* group, uint32_t lds, int lane)
+{
+#pragma unroll
+    for (int i = 0; i < D / 32; ++i) async_copy_1k_stream(group, (uint32_t)(i * 1024 + lane * 16), __builtin_amdgcn_readfirstlane(lds + i * 1024u));
+    async_copy_256(group, (uint32_t)(32 * D + min(lane * 4, paged_group_bytes(D) - 32 * D - 4)), __builtin_amdgcn_readfirstlane(lds + 32u * D));
+}
+
+template <int D> __device__ inline void load_group(GroupCodes<D>& c, const uint8_t* group, int m, int q)
 {
     if constexpr (D == 128) {
         c.k[0] = *(const u32x4_t*)(group + q * 512 + m * 16);
@@ -58,7 +71,12 @@ template <typename T, int D, int NT> __global__ __launch_bounds__(kFewWaves * 64
                                                                                                         T* __restrict__ out, float* __restrict__ part)
 {
     constexpr int kTerms = sizeof(T) == 2 ? 1 : 3, kSteps = D / 32;
-    __shared__ float o_wave[kFewWaves][16][D + 4], m_wave[kFewWaves][16], l_wave[kFewWaves][16];
+    constexpr int kStage = few_stage_bytes<D>(), kCopies = few_copies<D>();
+    typedef float WaveRows[16][D + 4];
+    __shared__ __attribute__((aligned(1024))) uint8_t ring[kFewWaves * kFewStages * kStage];      // afterwards: the waves' outputs
+    __shared__ float m_wave[kFewWaves][16], l_wave[kFewWaves][16];
+    static_assert(sizeof(WaveRows) <= kFewStages * kStage, "outputs fit the stages");
+    WaveRows* o_wave = (WaveRows*)ring;
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, m = lane & 15, qq = lane >> 4;
     const int split = blockIdx.x, hk = blockIdx.y, s = blockIdx.z;
     const SeqView v = seq_view(b, s);
@@ -105,24 +123,31 @@ template <typename T, int D, int NT> __global__ __launch_bounds__(kFewWaves * 64
 
     const int count = (last - first - wave + kFewWaves - 1) / kFewWaves;      // groups of this wave
     int numbers = -1;      // lane l: place of the wave's group 64 * k + l
-    GroupCodes<D> cur, next;
-    bool have = false;
-    auto fetch = [&](int i, GroupCodes<D>& c) -> bool {
-        if (i >= count) return false;
+    uint32_t missing = 0;      // bit: stage holds a group that does not exist (what was copied is page 0's)
+    const uint8_t* stages = ring + wave * kFewStages * kStage;
+    const uint32_t stages_lds = lds_address(stages);
+    auto issue = [&](int i) {
         if ((i & 63) == 0) {
             const int mine = i + lane;
-            const int64_t at = mine < count ? paged_group(g, b, s, (first + wave + mine * kFewWaves) * kGroupTokens) : -1;
-            numbers = (int)at;
+            numbers = mine < count ? (int)paged_group(g, b, s, (first + wave + mine * kFewWaves) * kGroupTokens) : -1;
         }
-        const int at = __builtin_amdgcn_readlane(numbers, i & 63);
-        if (at < 0) return false;
-        load_group<D>(c, g.pages + ((int64_t)at + hk * g.groups) * g.group_bytes, m, qq);
-        return true;
+        const int at = __builtin_amdgcn_readlane(numbers, i & 63), stage = i % kFewStages;
+        missing = at < 0 ? missing | 1u << stage : missing & ~(1u << stage);
+        copy_group<D>(g.pages + ((int64_t)max(at, 0) + hk * g.groups) * g.group_bytes, stages_lds + stage * kStage, lane);
     };
-    have = fetch(0, cur);
+    for (int i = 0; i < min(count, kFewStages - 1); ++i) issue(i);
     for (int i = 0; i < count; ++i) {
-        const bool have_next = fetch(i + 1, next);
-        if (have) {
+        wait_lds_reads();      // the stage that is filled now has been read
+        if (i + kFewStages - 1 < count) issue(i + kFewStages - 1);
+        const int behind = min(count - 1 - i, kFewStages - 1);      // groups on their way behind this one
+        if (behind == 3) wait_vm_fenced<3 * kCopies>();
+        else if (behind == 2) wait_vm_fenced<2 * kCopies>();
+        else if (behind == 1) wait_vm_fenced<kCopies>();
+        else wait_vm_fenced<0>();
+        static_assert(kFewStages == 4, "the waits are written for four stages");
+        if (!(missing >> (i % kFewStages) & 1u)) {
+            GroupCodes<D> cur;
+            load_group<D>(cur, stages + i % kFewStages * kStage, m, qq);
             const int key0 = (first + wave + i * kFewWaves) * kGroupTokens;
             const bool whole = key0 >= whole_from && key0 + 32 <= whole_to;
             f32x4_t st[NT][2];
@@ -197,9 +222,8 @@ template <typename T, int D, int NT> __global__ __launch_bounds__(kFewWaves * 64
                     }
             }
         }
-        cur = next;
-        have = have_next;
     }
+    __syncthreads();      // every wave has read its last stage
 
     // the waves' results together: a row's channels by 16 threads
     const bool alone = span.last - span.first <= per;      // no other split has keys
@@ -247,12 +271,12 @@ template <typename T, int D, int NT> __global__ __launch_bounds__(kFewWaves * 64
     }
 }
 
-// Joins the splits of a row: D/4 threads on four channels each, the splits over the rest of the workgroup.
+// Joins the splits of a row: the splits' maxima and sums a thread each, then D/4 threads on four channels with the splits over the rest of the workgroup.
 template <typename T, int D> __global__ __launch_bounds__(256) void merge_few_kernel(PagedGeom g, PagedBatch b, FewPlan plan, const float* __restrict__ part, T* __restrict__ out)
 {
     constexpr int kLanes = D / 4, kParts = 256 / kLanes;
-    __shared__ float o_part[kParts][D], l_part[kParts], m_part[kParts];
-    const int row = blockIdx.x, hk = blockIdx.y, s = blockIdx.z;
+    __shared__ float o_part[kParts][D], weight[kFewMaxSplits], m_wave[4], l_wave[4];
+    const int row = blockIdx.x, hk = blockIdx.y, s = blockIdx.z, tid = threadIdx.x;
     const SeqView v = seq_view(b, s);
     if (row >= v.n * g.G || v.n * g.G > plan.max_rows) return;
     const KeySpan span = key_span(g, b, v);
@@ -260,31 +284,46 @@ template <typename T, int D> __global__ __launch_bounds__(256) void merge_few_ke
     if (splits <= 1) return;      // written by its only split
     const float* x = part + ((int64_t)(s * g.Hkv + hk) * plan.splits * plan.max_rows + row) * (D + 2);
     const int64_t step = (int64_t)plan.max_rows * (D + 2);
-    const int p = threadIdx.x / kLanes, c = threadIdx.x % kLanes * 4;
-    float top = -INFINITY;
-    for (int i = p; i < splits; i += kParts) top = fmaxf(top, x[i * step + D]);
-    if (c == 0) m_part[p] = top;
+    // (at most kFewMaxSplits of them, two a thread)
+    float2 ml[2];
+#pragma unroll
+    for (int i = 0; i < 2; ++i) ml[i] = tid + 256 * i < splits ? *(const float2*)(x + (tid + 256 * i) * step + D) : make_float2(-INFINITY, 0.f);
+    float top = fmaxf(ml[0].x, ml[1].x);
+#pragma unroll
+    for (int w = 32; w; w >>= 1) top = fmaxf(top, __shfl_xor(top, w));
+    if ((tid & 63) == 0) m_wave[tid >> 6] = top;
     __syncthreads();
-    top = m_part[0];
+    top = fmaxf(fmaxf(m_wave[0], m_wave[1]), fmaxf(m_wave[2], m_wave[3]));
+    float l = 0.f;
 #pragma unroll
-    for (int i = 1; i < kParts; ++i) top = fmaxf(top, m_part[i]);
-    float l = 0.f, o[4] = {};
-    for (int i = p; i < splits; i += kParts) {
-        const float m = x[i * step + D], f = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m - top);
-        l += f * x[i * step + D + 1];
-#pragma unroll
-        for (int e = 0; e < 4; ++e) o[e] += f * x[i * step + c + e];
+    for (int i = 0; i < 2; ++i) {
+        const float f = ml[i].x == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(ml[i].x - top);
+        weight[tid + 256 * i] = f;
+        l += f * ml[i].y;
     }
-    if (c == 0) l_part[p] = l;
 #pragma unroll
-    for (int e = 0; e < 4; ++e) o_part[p][c + e] = o[e];
+    for (int w = 32; w; w >>= 1) l += __shfl_xor(l, w);
+    if ((tid & 63) == 0) l_wave[tid >> 6] = l;
+    __syncthreads();
+    const int p = tid / kLanes, c = tid % kLanes * 4;
+    float o[4] = {};
+#pragma unroll 8
+    for (int i = p; i < splits; i += kParts) {
+        const float f = weight[i];
+        const float2 a = *(const float2*)(x + i * step + c), e = *(const float2*)(x + i * step + c + 2);
+        o[0] += f * a.x;
+        o[1] += f * a.y;
+        o[2] += f * e.x;
+        o[3] += f * e.y;
+    }
+    *(float4*)&o_part[p][c] = make_float4(o[0], o[1], o[2], o[3]);
     __syncthreads();
     if (p) return;
-    l = 0.f;
-    for (int i = 0; i < kParts; ++i) l += l_part[i];
+    l = l_wave[0] + l_wave[1] + l_wave[2] + l_wave[3];
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
         o[e] = 0.f;
+#pragma unroll
         for (int i = 0; i < kParts; ++i) o[e] += o_part[i][c + e];
     }
     const int i = row / g.G, h = row - i * g.G;
@@ -293,24 +332,21 @@ template <typename T, int D> __global__ __launch_bounds__(256) void merge_few_ke
 }
 
 // ------------------------------------------------------------------ launches
-// Splits of a launch for few rows.  A share is a whole number of rounds of the workgroup's waves: at least one, at most 8, and
-// between them what makes about 1024 workgroups (four for each compute unit); more than 8 only where there would be more than kFewParts.
+// Splits of a launch for few rows: a share is a whole number of rounds of the workgroup's waves.  Two workgroups run on a compute unit, so 512 a
+// launch, or as many times that as leave a workgroup at most 24 rounds (sequences of different lengths even out over them).
 static FewPlan few_plan(const PagedGeom& g, const PagedBatch& b)
 {
     FewPlan p;
     const int64_t pairs = (int64_t)b.n_seqs * g.Hkv;
     const int longest = g.window && g.window < b.max_length - b.max_new ? g.window + b.max_new + 31 : b.max_length;
-    const int64_t groups = longest / kGroupTokens + 1;
-    int64_t rounds = groups * pairs / (1024 * kFewWaves);
-    rounds = rounds < 1 ? 1 : rounds > 8 ? 8 : rounds;
-    int64_t splits = (groups + rounds * kFewWaves - 1) / (rounds * kFewWaves);
-    const int64_t most = kFewParts / pairs < 1 ? 1 : kFewParts / pairs;
-    if (splits > most) {
-        splits = most;
-        rounds = (groups + splits * kFewWaves - 1) / (splits * kFewWaves);
-    }
-    p.groups_per_split = (int)(rounds * kFewWaves);
-    p.splits = (int)splits;
+    const int64_t rounds = (longest / kGroupTokens + kFewWaves) / kFewWaves;      // of the longest sequence
+    int64_t splits = 512 / pairs < 1 ? 1 : 512 / pairs;
+    for (int64_t k = 2; (rounds + splits - 1) / splits > 24 && 512 * k / pairs * pairs <= kFewParts; ++k) splits = 512 * k / pairs < 1 ? 1 : 512 * k / pairs;
+    if (splits > rounds) splits = rounds;
+    if (splits > kFewMaxSplits) splits = kFewMaxSplits;
+    const int64_t each = (rounds + splits - 1) / splits;
+    p.groups_per_split = (int)(each * kFewWaves);
+    p.splits = (int)((rounds + each - 1) / each);
     const int rows = b.max_new * g.G;
     p.max_rows = rows < kFewRows ? rows : kFewRows;
     return p;
