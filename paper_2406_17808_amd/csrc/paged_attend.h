@@ -51,6 +51,9 @@ __device__ inline KeySpan key_span(const PagedGeom& g, const PagedBatch& b, cons
     return k;
 }
 
+// The larger of two numbers, NaN if one is: an instruction of its own on gfx950 (fmaxf first makes its operands canonical, one instruction each).
+__device__ inline float max_of(float a, float b) { return __builtin_elementwise_maximum(a, b); }
+
 // The scale of a K block as the conversion takes it; NaN for byte 255.
 __device__ inline float scale_of_byte(uint32_t byte) { return __uint_as_float(byte == 255u ? 0x7FC00000u : byte << 23); }
 

@@ -1,4 +1,6 @@
 // Attention over the paged cache in 4 bits: a few query rows per KV head (single tokens, a few of them) against a long cache.
+#include <type_traits>
+
 #include "async_copy.h"
 #include "paged_attend.h"
 
@@ -67,7 +69,7 @@ __device__ inline float sum_quarters(float x)
     return __uint_as_float(s[0]) + __uint_as_float(s[1]);
 }
 
-template <typename T, int D, int NT> __global__ __launch_bounds__(kFewWaves * 64) void attend_few_kernel(PagedGeom g, PagedBatch b, FewPlan plan, const T* __restrict__ q, int64_t q_stride,
+template <typename T, int D, int NT> __global__ __launch_bounds__(kFewWaves * 64, sizeof(T) == 4 && NT == 2 ? 1 : 2) void attend_few_kernel(PagedGeom g, PagedBatch b, FewPlan plan, const T* __restrict__ q, int64_t q_stride,
                                                                                                         T* __restrict__ out, float* __restrict__ part)
 {
     constexpr int kTerms = sizeof(T) == 2 ? 1 : 3, kSteps = D / 32;
@@ -77,7 +79,7 @@ template <typename T, int D, int NT> __global__ __launch_bounds__(kFewWaves * 64
     __shared__ float m_wave[kFewWaves][16], l_wave[kFewWaves][16];
     static_assert(sizeof(WaveRows) <= kFewStages * kStage, "outputs fit the stages");
     WaveRows* o_wave = (WaveRows*)ring;
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, m = lane & 15, qq = lane >> 4;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), m = lane & 15, qq = lane >> 4;
     const int split = blockIdx.x, hk = blockIdx.y, s = blockIdx.z;
     const SeqView v = seq_view(b, s);
     const int rows = v.n * g.G;
@@ -166,47 +168,51 @@ template <typename T, int D, int NT> __global__ __launch_bounds__(kFewWaves * 64
                 }
             }
             Frag pf[NT][kTerms];
+            // SOME: there may be keys that a column does not see
+            auto probabilities = [&](auto some) {
 #pragma unroll
-            for (int n = 0; n < NT; ++n) {
-                uint32_t seen = 255;
-                if (!whole) {
-                    const int to = min(pos[n] + 1, b.max_length), from = g.window ? pos[n] - g.window + 1 : 0;
-                    seen = 0;
+                for (int n = 0; n < NT; ++n) {
+                    bool seen[8];
+                    if (decltype(some)::value) {
+                        const int to = min(pos[n] + 1, b.max_length), from = g.window ? pos[n] - g.window + 1 : 0;
+#pragma unroll
+                        for (int j = 0; j < 8; ++j) {
+                            const int key = key0 + 16 * (j >> 2) + 4 * qq + (j & 3);
+                            seen[j] = key >= from && key < to;
+                            if (!seen[j]) st[n][j >> 2][j & 3] = -INFINITY;
+                        }
+                    }
+                    float mx = st[n][0][0];
+#pragma unroll
+                    for (int j = 1; j < 8; ++j) mx = max_of(mx, st[n][j >> 2][j & 3]);
+                    mx *= scale;
+                    if (__ballot(mx > top[n] + kRescaleLog2)) {
+                        const float now = max_of(top[n], max_quarters(mx));
+                        const float shrink = now == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(top[n] - now);
+                        top[n] = now;
+                        sum[n] *= shrink;
+#pragma unroll
+                        for (int t = 0; t < D / 16; ++t) o[n][t] *= shrink;
+                    }
+                    float p[8];
 #pragma unroll
                     for (int j = 0; j < 8; ++j) {
-                        const int key = key0 + 16 * (j >> 2) + 4 * qq + (j & 3);
-                        if (key >= from && key < to) seen |= 1u << j;
-                        else st[n][j >> 2][j & 3] = -INFINITY;
+                        float e = __builtin_amdgcn_exp2f(__builtin_fmaf(st[n][j >> 2][j & 3], scale, -top[n]));
+                        if (decltype(some)::value) e = seen[j] ? e : 0.f;
+                        sum[n] += e;
+                        const uint32_t w = cur.scales[j >> 1];
+                        p[j] = e * __uint_as_float(j & 1 ? w & 0xFFFF0000u : w << 16);
+                        if (decltype(some)::value) p[j] = seen[j] ? p[j] : 0.f;      // what is not seen may hold any scale
+                    }
+#pragma unroll
+                    for (int x = 0; x < 4; ++x) {
+                        if constexpr (kTerms == 1) pf[n][0].u[x] = cvt_pk_bf16(p[x], p[4 + x]);
+                        else split_terms(p[x], p[4 + x], [&](int term, uint32_t pair) { pf[n][term].u[x] = pair; });
                     }
                 }
-                float mx = st[n][0][0];
-#pragma unroll
-                for (int j = 1; j < 8; ++j) mx = fmaxf(mx, st[n][j >> 2][j & 3]);
-                mx *= scale;
-                if (__ballot(mx > top[n] + kRescaleLog2)) {
-                    const float now = fmaxf(top[n], max_quarters(mx));
-                    const float shrink = now == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(top[n] - now);
-                    top[n] = now;
-                    sum[n] *= shrink;
-#pragma unroll
-                    for (int t = 0; t < D / 16; ++t) o[n][t] *= shrink;
-                }
-                float p[8];
-#pragma unroll
-                for (int j = 0; j < 8; ++j) {
-                    float e = __builtin_amdgcn_exp2f(__builtin_fmaf(st[n][j >> 2][j & 3], scale, -top[n]));
-                    if (!whole && !(seen >> j & 1u)) e = 0.f;
-                    sum[n] += e;
-                    const uint32_t w = cur.scales[j >> 1];
-                    const float vs = __uint_as_float(j & 1 ? w & 0xFFFF0000u : w << 16);
-                    p[j] = !whole && !(seen >> j & 1u) ? 0.f : e * vs;      // what is not seen may hold any scale
-                }
-#pragma unroll
-                for (int x = 0; x < 4; ++x) {
-                    if constexpr (kTerms == 1) pf[n][0].u[x] = cvt_pk_bf16(p[x], p[4 + x]);
-                    else split_terms(p[x], p[4 + x], [&](int term, uint32_t pair) { pf[n][term].u[x] = pair; });
-                }
-            }
+            };
+            if (whole) probabilities(std::false_type());
+            else probabilities(std::true_type());
 #pragma unroll
             for (int u = 0; u < D / 32; ++u) {
                 // four bytes of keys 4q + b and of keys 16 + 4q + b, two channels each -> eight keys of one channel

@@ -232,10 +232,10 @@ template <typename T, int D, int NW> __global__ __launch_bounds__(NW * 64, 1) vo
 #pragma unroll
         for (int kb = 0; kb < 2; ++kb)
 #pragma unroll
-            for (int j = 0; j < 16; ++j) mx = fmaxf(mx, st[kb][j]);
+            for (int j = 0; j < 16; ++j) mx = max_of(mx, st[kb][j]);
         mx *= scale;
         if (__ballot(mx > top + kRescaleLog2)) {
-            const float now = fmaxf(top, max_xor32(mx));
+            const float now = max_of(top, max_xor32(mx));
             const float shrink = now == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(top - now);
             top = now;
             sum *= shrink;
