@@ -17,9 +17,11 @@ namespace ckv {
 // (24 bits), with a product each.
 //
 // A workgroup has kFewWaves waves; wave w takes groups w, w + kFewWaves, ... of the workgroup's share.  A wave has kFewStages groups of its own in
-// LDS, filled by asynchronous copies (a group is contiguous), and waits only for its own: two workgroups on a compute unit have 120 KB on their way
-// whatever the waves compute.  (Loads to registers, one group ahead, three waves a SIMD: 50 KB, 4.3 TB/s.)  The running maximum is raised only
-// when a logit exceeds it by 2^8 (in 32 bits nothing is lost below 2^127): a vote instead of an exchange between lanes for most groups.
+// LDS, filled by asynchronous copies (a group is contiguous), and waits only for its own.  A group takes a wave 1 to 2 us from its first LDS read to its last product, most of it
+// waiting for itself, so waves a SIMD count for more than bytes on their way: 32 sequences of 16384 keys (562 MB) take 104 us with two
+// stages and three workgroups a compute unit, 106 with three stages, 114 with four and two workgroups; 132 with the next group's
+// loads in registers.  The running maximum is raised only when a logit exceeds it by 2^8 (in 32 bits nothing is lost below 2^127): a
+// vote instead of an exchange between lanes for most groups.
 template <int D> struct GroupCodes {
     u32x4_t k[2];            // D = 64: the first two words
     u32x4_t v[D / 64];
@@ -27,7 +29,7 @@ template <int D> struct GroupCodes {
     uint32_t exps;           // K bytes of keys m and 16 + m
 };
 
-constexpr int kFewStages = 4;
+constexpr int kFewStages = 2;
 template <int D> constexpr int few_stage_bytes() { return 32 * D + 256; }      // the codes, and 256 bytes from the scales on
 template <int D> constexpr int few_copies() { return D / 32 + 1; }             // copies of 1 KB, and one of 256 bytes
 
@@ -37,6 +39,17 @@ template <int D> __device__ inline void copy_group(const uint8_t* group, uint32_
 #pragma unroll
     for (int i = 0; i < D / 32; ++i) async_copy_1k_stream(group, (uint32_t)(i * 1024 + lane * 16), __builtin_amdgcn_readfirstlane(lds + i * 1024u));
     async_copy_256(group, (uint32_t)(32 * D + min(lane * 4, paged_group_bytes(D) - 32 * D - 4)), __builtin_amdgcn_readfirstlane(lds + 32u * D));
+}
+
+// At most `behind` groups (0 .. MOST) of C copies each on their way.
+template <int MOST, int C> __device__ inline void wait_behind(int behind)
+{
+    if constexpr (MOST == 0) {
+        wait_vm_fenced<0>();
+    } else {
+        if (behind == MOST) wait_vm_fenced<MOST * C>();
+        else wait_behind<MOST - 1, C>(behind);
+    }
 }
 
 template <int D> __device__ inline void load_group(GroupCodes<D>& c, const uint8_t* group, int m, int q)
@@ -142,11 +155,7 @@ template <typename T, int D, int NT> __global__ __launch_bounds__(kFewWaves * 64
         wait_lds_reads();      // the stage that is filled now has been read
         if (i + kFewStages - 1 < count) issue(i + kFewStages - 1);
         const int behind = min(count - 1 - i, kFewStages - 1);      // groups on their way behind this one
-        if (behind == 3) wait_vm_fenced<3 * kCopies>();
-        else if (behind == 2) wait_vm_fenced<2 * kCopies>();
-        else if (behind == 1) wait_vm_fenced<kCopies>();
-        else wait_vm_fenced<0>();
-        static_assert(kFewStages == 4, "the waits are written for four stages");
+        wait_behind<kFewStages - 1, kCopies>(behind);
         if (!(missing >> (i % kFewStages) & 1u)) {
             GroupCodes<D> cur;
             load_group<D>(cur, stages + i % kFewStages * kStage, m, qq);
@@ -338,16 +347,19 @@ template <typename T, int D> __global__ __launch_bounds__(256) void merge_few_ke
 }
 
 // ------------------------------------------------------------------ launches
-// Splits of a launch for few rows: a share is a whole number of rounds of the workgroup's waves.  Two workgroups run on a compute unit, so 512 a
-// launch, or as many times that as leave a workgroup at most 24 rounds (sequences of different lengths even out over them).
+// Splits of a launch for few rows: a share is a whole number of rounds of the workgroup's waves.  A compute unit runs three workgroups (registers; four at D =
+// 64), so that many times 256 a launch, or as many times that as leave a workgroup at most 24 rounds (sequences of different lengths even out over them: 32
+// of up to 16384 keys take 61 us, with 48 rounds 90, with 12 77).
+constexpr int kFewRounds = 24;
 static FewPlan few_plan(const PagedGeom& g, const PagedBatch& b)
 {
     FewPlan p;
     const int64_t pairs = (int64_t)b.n_seqs * g.Hkv;
     const int longest = g.window && g.window < b.max_length - b.max_new ? g.window + b.max_new + 31 : b.max_length;
     const int64_t rounds = (longest / kGroupTokens + kFewWaves) / kFewWaves;      // of the longest sequence
-    int64_t splits = 512 / pairs < 1 ? 1 : 512 / pairs;
-    for (int64_t k = 2; (rounds + splits - 1) / splits > 24 && 512 * k / pairs * pairs <= kFewParts; ++k) splits = 512 * k / pairs < 1 ? 1 : 512 * k / pairs;
+    const int64_t fill = g.d == 64 ? 1024 : 768;
+    int64_t splits = fill / pairs < 1 ? 1 : fill / pairs;
+    for (int64_t k = 2; (rounds + splits - 1) / splits > kFewRounds && fill * k / pairs * pairs <= kFewParts; ++k) splits = fill * k / pairs < 1 ? 1 : fill * k / pairs;
     if (splits > rounds) splits = rounds;
     if (splits > kFewMaxSplits) splits = kFewMaxSplits;
     const int64_t each = (rounds + splits - 1) / splits;
