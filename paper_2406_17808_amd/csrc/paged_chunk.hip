@@ -21,6 +21,22 @@ namespace ckv {
 // 2x + 1, and set x + 2 is written from phase 2x + 2 on: two stages do.
 // NW = 4 (fp32: queries and scaled probabilities are sums of three bf16 terms, three times the products and the query registers): all waves are early and convert
 // K and V.
+
+// What a thread converts: N words of codes, and the K byte or a V scale.
+template <int N> struct Piece {
+    uint32_t w[N], extra;
+    __device__ void load(const uint8_t* p)
+    {
+        if constexpr (N == 4) {
+            const u32x4_t c = *(const u32x4_t*)p;
+            w[0] = c[0]; w[1] = c[1]; w[2] = c[2]; w[3] = c[3];
+        } else {
+            const uint2 c = *(const uint2*)p;
+            w[0] = c.x; w[1] = c.y;
+        }
+    }
+};
+
 template <typename T, int D, int NW> __global__ __launch_bounds__(NW * 64, 1) void attend_chunk_kernel(PagedGeom g, PagedBatch b, ChunkPlan plan, const T* __restrict__ q, int64_t q_stride,
                                                                                                    T* __restrict__ out, float* __restrict__ part)
 {
@@ -29,6 +45,7 @@ template <typename T, int D, int NW> __global__ __launch_bounds__(NW * 64, 1) vo
     constexpr int kWords = D / 32;                     // words of codes a piece has: 8 * kWords channels of a key, or 8 keys of kWords channels
     __shared__ __attribute__((aligned(16))) bf16_t k_lds[2][kBN * D], v_lds[2][kBN * D];
     __shared__ __attribute__((aligned(16))) float vs_lds[2][kBN];
+    __shared__ uint32_t odd_lds[2][2];      // by group and V slot: the row's scale is an infinity or NaN
 
     const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), l = tid & 63, l32 = l & 31, half = l >> 5;
     const bool late = NW == 8 && wave >= 4;
@@ -72,11 +89,16 @@ template <typename T, int D, int NW> __global__ __launch_bounds__(NW * 64, 1) vo
             }
         }
     }
+    wait_vm_fenced<0>();      // (or the products wait for the codes on their way as well)
     f32x16_t o[DB], st[2];
 #pragma unroll
     for (int db = 0; db < DB; ++db)
 #pragma unroll
         for (int j = 0; j < 16; ++j) o[db][j] = 0.f;
+#pragma unroll
+    for (int kb = 0; kb < 2; ++kb)
+#pragma unroll
+        for (int j = 0; j < 16; ++j) st[kb][j] = 0.f;
     float top = -INFINITY, sum = 0.f;
     const float scale = g.scale * 1.44269504088896341f;
 
@@ -88,134 +110,133 @@ template <typename T, int D, int NW> __global__ __launch_bounds__(NW * 64, 1) vo
     }
     missing = __syncthreads_or(missing);
 
-    // ---- codes -> LDS.  Piece kind 0: K, waves 0 - 3 of eight; kind 1: V.  A wave's pieces are of one group of the tile.
-    struct Piece {
-        uint32_t w[kWords];
-        uint32_t extra;      // K: the exponent byte; V: the bits of a scale
-    };
+    // ---- codes -> LDS
     // item i of a wave is pieces 64 (w % 2) .. of group w / 2 % 2, w = wave + NW * i; K for w < 4
-    auto load_piece = [&](int item, int tile, Piece& x) {
-        const int w = wave + NW * item, gi = (w & 3) >> 1;      // group of the tile
-        const int64_t at = paged_group(g, b, s, ((tile0 + tile) * 2 + gi) * kGroupTokens);
-        const uint8_t* group = g.pages + ((at < 0 ? 0 : at) + (int64_t)hk * g.groups) * g.group_bytes;
-        const int n = (w & 1) * 64 + l;      // piece of the group, 0 .. 127
-        if (w < 4) {
-            if constexpr (D == 128) {      // block n / 32 of key n % 32
-                const u32x4_t c = *(const u32x4_t*)(group + n * 16);
-                x.w[0] = c[0]; x.w[1] = c[1]; x.w[2] = c[2]; x.w[3] = c[3];
-                x.extra = group[k_exp_byte(D, n >> 5, n & 31)];
-            } else {                       // half n % 2 of block n / 64 of key n / 2 % 32
-                const uint2 c = *(const uint2*)(group + n * 8);
-                x.w[0] = c.x; x.w[1] = c.y;
-                x.extra = group[k_exp_byte(D, n >> 6, (n >> 1) & 31)];
-            }
-        } else {
-            if constexpr (D == 128) {
-                const u32x4_t c = *(const u32x4_t*)(group + 16 * D + n * 16);
-                x.w[0] = c[0]; x.w[1] = c[1]; x.w[2] = c[2]; x.w[3] = c[3];
-            } else {
-                const uint2 c = *(const uint2*)(group + 16 * D + n * 8);
-                x.w[0] = c.x; x.w[1] = c.y;
-            }
-            if ((w & 1) == 0 && l < 32) x.extra = at < 0 ? 0u : (uint32_t)*(const uint16_t*)(group + 33 * D + 2 * l) << 16;
-        }
-    };
-    auto write_piece = [&](int item, int stage, const Piece& x) {
-        const int w = wave + NW * item, gi = (w & 3) >> 1, n = (w & 1) * 64 + l;
-        if (w < 4) {
-            const float ks = scale_of_byte(x.extra);
-            const int r = 32 * gi + (D == 128 ? n & 31 : (n >> 1) & 31);
-            const int piece = D == 128 ? 4 * (n >> 5) : 4 * (n >> 6) + 2 * (n & 1);      // 8 channels each
-#pragma unroll
-            for (int e = 0; e < kWords; ++e) *(u32x4_t*)&k_lds[stage][r * D + ((piece + e) ^ (r & 7)) * 8] = bf16_of_codes(x.w[e], ks).u;
-        } else {
-            // D = 128: chunk n / 64, keys 4q + b, 16 + 4q + b with q = n / 16 % 4, channels n % 16 + 16 (0 .. 3) of 64; D = 64: half of that
-            const int c16 = D == 128 ? n : n >> 1, ch0 = (D == 128 ? 64 * (n >> 6) : 32 * (n & 1)) + (c16 & 15), quarter = (c16 >> 4) & 3;
-#pragma unroll
-            for (int e = 0; e < kWords; e += 2) {
-                const uint32_t a = x.w[e], c = x.w[e + 1];
-                const uint32_t lo = (a & 0x0F0F0F0Fu) | ((c << 4) & 0xF0F0F0F0u), hi = ((a >> 4) & 0x0F0F0F0Fu) | (c & 0xF0F0F0F0u);
-                const int ch = ch0 + 16 * e;
-                *(u32x4_t*)&v_lds[stage][ch * kBN + ((4 * gi + quarter) ^ (ch & 7)) * 8] = bf16_of_codes(lo, 1.f).u;
-                *(u32x4_t*)&v_lds[stage][(ch + 16) * kBN + ((4 * gi + quarter) ^ (ch & 7)) * 8] = bf16_of_codes(hi, 1.f).u;
-            }
-            if ((w & 1) == 0 && l < 32) vs_lds[stage][32 * gi + l] = __uint_as_float(x.extra);
-        }
-    };
     auto tile_of = [&](int item, int set) { return wave + NW * item < 4 ? set + 1 : set; };
-    Piece held[kItems];
+    Piece<kWords> held[kItems];
+    int numbers[kItems];      // lane l: place of the item's group in tile 64 * k + l
     auto load_set = [&](int set) {
 #pragma unroll
         for (int i = 0; i < kItems; ++i) {
-            const int t = tile_of(i, set);
-            if (t >= 0 && t < NT) load_piece(i, t, held[i]);
+            const int t = tile_of(i, set), w = wave + NW * i, gi = (w & 3) >> 1;
+            if (t < 0 || t >= NT) continue;
+            if ((t & 63) == 0) numbers[i] = t + l < NT ? (int)paged_group(g, b, s, ((tile0 + t + l) * 2 + gi) * kGroupTokens) : -1;
+            const int at = __builtin_amdgcn_readlane(numbers[i], t & 63), n = (w & 1) * 64 + l;      // piece of the group, 0 .. 127
+            const uint8_t* group = g.pages + ((int64_t)max(at, 0) + hk * g.groups) * g.group_bytes;
+            held[i].load(group + (w < 4 ? 0 : 16 * D) + n * (4 * kWords));
+            if (w < 4) held[i].extra = group[D == 128 ? k_exp_byte(D, n >> 5, n & 31) : k_exp_byte(D, n >> 6, (n >> 1) & 31)];
+            else if ((w & 1) == 0) held[i].extra = *(const uint16_t*)(group + 33 * D + 2 * l32);
         }
     };
     auto write_set = [&](int set) {
+        const int stage = set & 1;
 #pragma unroll
         for (int i = 0; i < kItems; ++i) {
-            const int t = tile_of(i, set);
-            if (t >= 0 && t < NT) write_piece(i, set & 1, held[i]);
+            const int t = tile_of(i, set), w = wave + NW * i, gi = (w & 3) >> 1, n = (w & 1) * 64 + l;
+            if (t < 0 || t >= NT) continue;
+            const Piece<kWords>& x = held[i];
+            if (w < 4) {
+                // D = 128: block n / 32 of key n % 32; D = 64: half n % 2 of block n / 64 of key n / 2 % 32
+                const float ks = scale_of_byte(x.extra);
+                const int r = 32 * gi + (D == 128 ? n & 31 : (n >> 1) & 31);
+                const int piece = D == 128 ? 4 * (n >> 5) : 4 * (n >> 6) + 2 * (n & 1);      // 8 channels each
+#pragma unroll
+                for (int e = 0; e < kWords; ++e) *(u32x4_t*)&k_lds[stage][r * D + ((piece + e) ^ (r & 7)) * 8] = bf16_of_codes(x.w[e], ks).u;
+            } else {
+                // D = 128: chunk n / 64, keys 4q + b, 16 + 4q + b with q = n / 16 % 4, channels n % 16 + 16 (0 .. 3) of 64; D = 64: half of that
+                const int c16 = D == 128 ? n : n >> 1, ch0 = (D == 128 ? 64 * (n >> 6) : 32 * (n & 1)) + (c16 & 15), quarter = (c16 >> 4) & 3;
+#pragma unroll
+                for (int e = 0; e < kWords; e += 2) {
+                    const uint32_t a = x.w[e], c = x.w[e + 1];
+                    const uint32_t lo = (a & 0x0F0F0F0Fu) | ((c << 4) & 0xF0F0F0F0u), hi = ((a >> 4) & 0x0F0F0F0Fu) | (c & 0xF0F0F0F0u);
+                    const int ch = ch0 + 16 * e;
+                    *(u32x4_t*)&v_lds[stage][ch * kBN + ((4 * gi + quarter) ^ (ch & 7)) * 8] = bf16_of_codes(lo, 1.f).u;
+                    *(u32x4_t*)&v_lds[stage][(ch + 16) * kBN + ((4 * gi + quarter) ^ (ch & 7)) * 8] = bf16_of_codes(hi, 1.f).u;
+                }
+                if ((w & 1) == 0) {
+                    // a NaN must not reach rows that do not see the key (0 * NaN): the scale becomes 0, and rows that do see it are marked
+                    const bool finite = (x.extra & 0x7F80u) != 0x7F80u;
+                    const uint32_t odd = (uint32_t)__ballot(!finite);      // lanes 32 .. 63 have the same scales
+                    if (l < 32) vs_lds[stage][32 * gi + l] = finite ? __uint_as_float(x.extra << 16) : 0.f;
+                    if (l == 0) odd_lds[stage][gi] = odd;
+                }
+            }
         }
     };
 
     // ---- blocks
-    auto active = [&](int t) { return (tile0 + t) * kBN < any_to && (tile0 + t + 1) * kBN > any_from; };
     auto whole = [&](int t) { return (tile0 + t) * kBN >= whole_from && (tile0 + t + 1) * kBN <= whole_to && !missing; };      // all rows of the wave see all keys
-    // SOME: rows may not see every key.  A key's scale may be NaN: it must not reach the rows that do not see the key.
-    auto values_block = [&](int stage, auto some) {
+    // Fragments of a matrix block, in the order of its products: 4 DB of V (16 keys of 32 channels), then 2 KS of K (16 channels of 32 keys).  Each
+    // is read kAhead products before it is used, the first ones (of V) in the vector block before.
+    constexpr int NV = 4 * DB, NF = NV + 2 * KS, kAhead = 8;
+    const bf16_t* v_lane[4];      // V piece 2 (2 gi + sx) + half of row l32, stage 0
+    const bf16_t* k_lane[KS];
 #pragma unroll
-            for (int gi = 0; gi < 2; ++gi)
+    for (int x = 0; x < 4; ++x) v_lane[x] = &v_lds[0][l32 * kBN + ((2 * x + half) ^ (l32 & 7)) * 8];
 #pragma unroll
-                for (int sx = 0; sx < 2; ++sx) {
-                    const float4 s0 = *(const float4*)&vs_lds[stage][32 * gi + 8 * (2 * sx + half)], s1 = *(const float4*)&vs_lds[stage][32 * gi + 8 * (2 * sx + half) + 4];
-                    const float a[4] = {s0.x, s0.y, s0.z, s0.w}, c[4] = {s1.x, s1.y, s1.z, s1.w};
-                    Frag pf[kTerms];
-#pragma unroll
-                    for (int x = 0; x < 4; ++x) {
-                        float p0 = st[gi][4 * sx + x] * a[x], p1 = st[gi][8 + 4 * sx + x] * c[x];
-                        if (decltype(some)::value) {
-                            p0 = st[gi][4 * sx + x] == 0.f ? 0.f : p0;
-                            p1 = st[gi][8 + 4 * sx + x] == 0.f ? 0.f : p1;
-                        }
-                        if constexpr (kTerms == 1) pf[0].u[x] = cvt_pk_bf16(p0, p1);
-                        else split_terms(p0, p1, [&](int term, uint32_t pair) { pf[term].u[x] = pair; });
-                    }
-#pragma unroll
-                    for (int db = 0; db < DB; ++db) {
-                        const int ch = 32 * db + l32;
-                        Frag vf;
-                        vf.u = *(const u32x4_t*)&v_lds[stage][ch * kBN + ((4 * gi + 2 * sx + half) ^ (ch & 7)) * 8];
-#pragma unroll
-                        for (int y = 0; y < kTerms; ++y) o[db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf.v, pf[y].v, o[db], 0, 0, 0);
-                    }
-                }
+    for (int ks = 0; ks < KS; ++ks) k_lane[ks] = &k_lds[0][l32 * D + ((2 * ks + half) ^ (l32 & 7)) * 8];
+    auto read_frag = [&](int stage, int i) {
+        Frag f;
+        if (i < NV) f.u = *(const u32x4_t*)(v_lane[i / DB] + stage * (kBN * D) + (i % DB) * (32 * kBN));
+        else f.u = *(const u32x4_t*)(k_lane[(i - NV) >> 1] + stage * (kBN * D) + ((i - NV) & 1) * (32 * D));
+        return f;
     };
+    Frag fr[kAhead];
+    auto read_ahead = [&](int t) {
+#pragma unroll
+        for (int i = 0; i < kAhead; ++i) fr[i] = read_frag(t & 1, i);
+    };
+    // probabilities of keys 16 x .. of the tile (in the order of V's pieces) times their V scales
+    auto scaled = [&](int stage, int x, Frag (&pf)[kTerms]) {
+        const float4 s0 = *(const float4*)&vs_lds[stage][8 * (2 * x + half)], s1 = *(const float4*)&vs_lds[stage][8 * (2 * x + half) + 4];
+        const float a[4] = {s0.x, s0.y, s0.z, s0.w}, c[4] = {s1.x, s1.y, s1.z, s1.w};
+        const int gi = x >> 1, sx = x & 1;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            const float p0 = st[gi][4 * sx + e] * a[e], p1 = st[gi][8 + 4 * sx + e] * c[e];
+            if constexpr (kTerms == 1) pf[0].u[e] = cvt_pk_bf16(p0, p1);
+            else split_terms(p0, p1, [&](int term, uint32_t pair) { pf[term].u[e] = pair; });
+        }
+    };
+    // P V of tile t (its first fragments are in fr), K Q^T of tile t + 1.  One form for all tiles: before a wave's first tile the probabilities are 0
+    // and V finite, behind its last nobody looks at the logits.  (Forms without the one or the other cost copies of all outputs where they meet.)
     auto matrix_block = [&](int t) {
         const int stage = t & 1;
-        if (t >= 0 && active(t)) {
-            if (whole(t)) values_block(stage, std::false_type());
-            else values_block(stage, std::true_type());
-        }
-        if (t + 1 < NT && active(t + 1)) {
+        Frag pf[2][kTerms];
+        scaled(stage, 0, pf[0]);
+        __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-            for (int kb = 0; kb < 2; ++kb)
+        for (int i = 0; i < NF; ++i) {
+            const Frag f = fr[i % kAhead];
+            if (i < NV) {
+                const int x = i / DB;
 #pragma unroll
-                for (int j = 0; j < 16; ++j) st[kb][j] = 0.f;
+                for (int y = 0; y < kTerms; ++y) o[i % DB] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(f.v, pf[x & 1][y].v, o[i % DB], 0, 0, 0);
+                if (i % DB == 0 && x < 3) scaled(stage, x + 1, pf[(x + 1) & 1]);
+            } else {
+                const int ks = (i - NV) >> 1, kb = (i - NV) & 1;
+                if (ks == 0)
 #pragma unroll
-            for (int ks = 0; ks < KS; ++ks)
+                    for (int j = 0; j < 16; ++j) st[kb][j] = 0.f;
 #pragma unroll
-                for (int kb = 0; kb < 2; ++kb) {
-                    const int r = 32 * kb + l32;
-                    Frag kf;
-                    kf.u = *(const u32x4_t*)&k_lds[stage][r * D + ((2 * ks + half) ^ (r & 7)) * 8];
-#pragma unroll
-                    for (int y = 0; y < kTerms; ++y) st[kb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf.v, qf[y][ks].v, st[kb], 0, 0, 0);
-                }
+                for (int y = 0; y < kTerms; ++y) st[kb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(f.v, qf[y][ks].v, st[kb], 0, 0, 0);
+            }
+            if (i + kAhead < NF) fr[i % kAhead] = read_frag(stage, i + kAhead);
+            __builtin_amdgcn_sched_barrier(0);
         }
     };
+    // a row that sees a key whose V row is NaN
+    auto mark_odd = [&](int t) {
+        const uint32_t odd[2] = {odd_lds[t & 1][0], odd_lds[t & 1][1]};
+        if (!__builtin_amdgcn_readfirstlane(odd[0] | odd[1])) return;
+#pragma unroll
+        for (int kb = 0; kb < 2; ++kb)
+            for (int r = 4 * half; r < 32; r += (r & 3) == 3 ? 5 : 1) {      // the lane's keys
+                const int key = (tile0 + t) * kBN + 32 * kb + r;
+                if ((odd[kb] >> v_slot(r) & 1u) && key >= from && key < to && !(missing && paged_group(g, b, s, key) < 0)) sum = __uint_as_float(0x7FC00000u);
+            }
+    };
     auto softmax = [&](int t) {
-        if (!active(t)) return;
         const int key0 = (tile0 + t) * kBN;
         if (!whole(t)) {
 #pragma unroll
@@ -253,31 +274,40 @@ template <typename T, int D, int NW> __global__ __launch_bounds__(NW * 64, 1) vo
                 sum += st[kb][j];
             }
     };
-    auto barrier = [&]() {
-        wait_lds_reads();      // what this wave has written to LDS is there
-        wg_barrier();
-    };
 
     // ---- the tiles.  A wave converts set t + lead in vector block t + 1.
     const int lead = late ? 2 : 1;
+    for (int i = tid; i < kBN * D / 8; i += NW * 64) *(u32x4_t*)&v_lds[1][8 * i] = u32x4_t{0, 0, 0, 0};      // matrix block -1 multiplies them with 0
+    if (tid < kBN) vs_lds[1][tid] = 0.f;
+    if (tid < 2) odd_lds[1][tid] = 0;
     for (int set = -1; set < lead - 1; ++set) {
         load_set(set);
         write_set(set);
     }
     load_set(lead - 1);
-    barrier();
-    if (late) barrier();
+    // the tiles that some row of the wave sees
+    const int a0 = max(any_from / kBN - tile0, 0), a1 = min((any_to + kBN - 1) / kBN - tile0, NT);
+    wait_lds_reads();
+    wg_barrier();
+    if (late) wg_barrier();
+    if (NW == 8 && a0 == 0) read_ahead(-1);
     for (int t = -1; t < NT; ++t) {
-        matrix_block(t);
-        barrier();
+        if (t >= a0 - 1 && t < a1) {
+            if (NW == 4) read_ahead(t);      // (V of the tile is written in the vector block before)
+            mark_odd(t);
+            matrix_block(t);
+        }
+        wg_barrier();      // (all that this wave has read from LDS is in the products)
         if (t + 1 < NT) {
+            if (t + 1 >= a0 && t + 1 < a1) softmax(t + 1);
             write_set(t + lead);
             load_set(t + lead + 1);
-            softmax(t + 1);
+            wait_lds_reads();      // what this wave has written is there
+            if (NW == 8) read_ahead(t + 1);
         }
-        barrier();
+        wg_barrier();
     }
-    if (!late && NW == 8) barrier();
+    if (!late && NW == 8) wg_barrier();
 
     // ---- rows out: lane l has channels 32 db + 8 (j / 4) + 4 half + j % 4 of its row
     const auto both = __builtin_amdgcn_permlane32_swap(__float_as_uint(sum), __float_as_uint(sum), false, false);
