@@ -12,7 +12,6 @@ namespace ckv {
 // codes of a tile of 64 keys (two groups) are turned into bf16 once per workgroup, on their way from registers to LDS: every
 // value is exact.  K: rows of D channels.  V: rows of 64 keys, in the order that the groups store them and the accumulators of S^T have them
 // (a lane's keys 8s + 4h + b and 16 + 8s + 4h + b are piece 2s + h of a group); a key's V scale multiplies its probability.
-// 16-byte pieces are XOR-swizzled with the row, so that eight lanes that read or write a column of rows meet eight different sets of banks.
 //
 // NW = 8: the two waves of a SIMD work in opposite phase, one on products (a matrix block: P V of tile t, then K Q^T of tile
 // t + 1) while the other takes exponentials and converts codes (a vector block), with a barrier between phases.  Set x in LDS is K of
@@ -36,6 +35,10 @@ template <int N> struct Piece {
         }
     }
 };
+
+// Positions of 16-byte pieces in the rows of a tile: sixteen lanes that read or write one column of sixteen rows meet all banks once (256 bytes).
+template <int D> __device__ inline int k_place(int r, int piece) { return r * D + (piece ^ (D == 128 ? r & 15 : (r >> 1) & 7)) * 8; }
+__device__ inline int v_place(int ch, int piece) { return ch * kBN + (piece ^ ((ch >> 1) & 7)) * 8; }
 
 template <typename T, int D, int NW> __global__ __launch_bounds__(NW * 64, 1) void attend_chunk_kernel(PagedGeom g, PagedBatch b, ChunkPlan plan, const T* __restrict__ q, int64_t q_stride,
                                                                                                    T* __restrict__ out, float* __restrict__ part)
@@ -141,7 +144,7 @@ template <typename T, int D, int NW> __global__ __launch_bounds__(NW * 64, 1) vo
                 const int r = 32 * gi + (D == 128 ? n & 31 : (n >> 1) & 31);
                 const int piece = D == 128 ? 4 * (n >> 5) : 4 * (n >> 6) + 2 * (n & 1);      // 8 channels each
 #pragma unroll
-                for (int e = 0; e < kWords; ++e) *(u32x4_t*)&k_lds[stage][r * D + ((piece + e) ^ (r & 7)) * 8] = bf16_of_codes(x.w[e], ks).u;
+                for (int e = 0; e < kWords; ++e) *(u32x4_t*)&k_lds[stage][k_place<D>(r, piece + e)] = bf16_of_codes(x.w[e], ks).u;
             } else {
                 // D = 128: chunk n / 64, keys 4q + b, 16 + 4q + b with q = n / 16 % 4, channels n % 16 + 16 (0 .. 3) of 64; D = 64: half of that
                 const int c16 = D == 128 ? n : n >> 1, ch0 = (D == 128 ? 64 * (n >> 6) : 32 * (n & 1)) + (c16 & 15), quarter = (c16 >> 4) & 3;
@@ -150,8 +153,8 @@ template <typename T, int D, int NW> __global__ __launch_bounds__(NW * 64, 1) vo
                     const uint32_t a = x.w[e], c = x.w[e + 1];
                     const uint32_t lo = (a & 0x0F0F0F0Fu) | ((c << 4) & 0xF0F0F0F0u), hi = ((a >> 4) & 0x0F0F0F0Fu) | (c & 0xF0F0F0F0u);
                     const int ch = ch0 + 16 * e;
-                    *(u32x4_t*)&v_lds[stage][ch * kBN + ((4 * gi + quarter) ^ (ch & 7)) * 8] = bf16_of_codes(lo, 1.f).u;
-                    *(u32x4_t*)&v_lds[stage][(ch + 16) * kBN + ((4 * gi + quarter) ^ (ch & 7)) * 8] = bf16_of_codes(hi, 1.f).u;
+                    *(u32x4_t*)&v_lds[stage][v_place(ch, 4 * gi + quarter)] = bf16_of_codes(lo, 1.f).u;
+                    *(u32x4_t*)&v_lds[stage][v_place(ch + 16, 4 * gi + quarter)] = bf16_of_codes(hi, 1.f).u;
                 }
                 if ((w & 1) == 0) {
                     // a NaN must not reach rows that do not see the key (0 * NaN): the scale becomes 0, and rows that do see it are marked
@@ -172,9 +175,9 @@ template <typename T, int D, int NW> __global__ __launch_bounds__(NW * 64, 1) vo
     const bf16_t* v_lane[4];      // V piece 2 (2 gi + sx) + half of row l32, stage 0
     const bf16_t* k_lane[KS];
 #pragma unroll
-    for (int x = 0; x < 4; ++x) v_lane[x] = &v_lds[0][l32 * kBN + ((2 * x + half) ^ (l32 & 7)) * 8];
+    for (int x = 0; x < 4; ++x) v_lane[x] = &v_lds[0][v_place(l32, 2 * x + half)];      // (rows 32 apart have the same order)
 #pragma unroll
-    for (int ks = 0; ks < KS; ++ks) k_lane[ks] = &k_lds[0][l32 * D + ((2 * ks + half) ^ (l32 & 7)) * 8];
+    for (int ks = 0; ks < KS; ++ks) k_lane[ks] = &k_lds[0][k_place<D>(l32, 2 * ks + half)];
     auto read_frag = [&](int stage, int i) {
         Frag f;
         if (i < NV) f.u = *(const u32x4_t*)(v_lane[i / DB] + stage * (kBN * D) + (i % DB) * (32 * kBN));
@@ -295,7 +298,9 @@ template <typename T, int D, int NW> __global__ __launch_bounds__(NW * 64, 1) vo
         if (t >= a0 - 1 && t < a1) {
             if (NW == 4) read_ahead(t);      // (V of the tile is written in the vector block before)
             mark_odd(t);
+            __builtin_amdgcn_s_setprio(1);
             matrix_block(t);
+            __builtin_amdgcn_s_setprio(0);
         }
         wg_barrier();      // (all that this wave has read from LDS is in the products)
         if (t + 1 < NT) {
