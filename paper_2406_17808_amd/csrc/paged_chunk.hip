@@ -24,6 +24,7 @@ namespace ckv {
 // What a thread converts: N words of codes, and the K byte or a V scale.
 template <int N> struct Piece {
     uint32_t w[N], extra;
+    bool gone;      // the group is missing: this is page 0's
     __device__ void load(const uint8_t* p)
     {
         if constexpr (N == 4) {
@@ -48,7 +49,7 @@ template <typename T, int D, int NW> __global__ __launch_bounds__(NW * 64, 1) vo
     constexpr int kWords = D / 32;                     // words of codes a piece has: 8 * kWords channels of a key, or 8 keys of kWords channels
     __shared__ __attribute__((aligned(16))) bf16_t k_lds[2][kBN * D], v_lds[2][kBN * D];
     __shared__ __attribute__((aligned(16))) float vs_lds[2][kBN];
-    __shared__ uint32_t odd_lds[2][2];      // by group and V slot: the row's scale is an infinity or NaN
+    __shared__ uint32_t odd_lds[2][2], gone_lds[2][2];      // of a group: bits of V slots whose scale is an infinity or NaN; whether the group is missing
 
     const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), l = tid & 63, l32 = l & 31, half = l >> 5;
     const bool late = NW == 8 && wave >= 4;
@@ -105,14 +106,6 @@ template <typename T, int D, int NW> __global__ __launch_bounds__(NW * 64, 1) vo
     float top = -INFINITY, sum = 0.f;
     const float scale = g.scale * 1.44269504088896341f;
 
-    // whether a group is missing anywhere in the range: then every tile looks for itself
-    bool missing = false;
-    for (int i = tid; i < 2 * NT; i += NW * 64) {
-        const int p = (2 * tile0 + i) * kGroupTokens;
-        missing |= p < to_of(pos_of(row0 + kRows - 1)) && paged_group(g, b, s, p) < 0;
-    }
-    missing = __syncthreads_or(missing);
-
     // ---- codes -> LDS
     // item i of a wave is pieces 64 (w % 2) .. of group w / 2 % 2, w = wave + NW * i; K for w < 4
     auto tile_of = [&](int item, int set) { return wave + NW * item < 4 ? set + 1 : set; };
@@ -129,6 +122,7 @@ template <typename T, int D, int NW> __global__ __launch_bounds__(NW * 64, 1) vo
             held[i].load(group + (w < 4 ? 0 : 16 * D) + n * (4 * kWords));
             if (w < 4) held[i].extra = group[D == 128 ? k_exp_byte(D, n >> 5, n & 31) : k_exp_byte(D, n >> 6, (n >> 1) & 31)];
             else if ((w & 1) == 0) held[i].extra = *(const uint16_t*)(group + 33 * D + 2 * l32);
+            held[i].gone = at < 0;
         }
     };
     auto write_set = [&](int set) {
@@ -145,6 +139,7 @@ template <typename T, int D, int NW> __global__ __launch_bounds__(NW * 64, 1) vo
                 const int piece = D == 128 ? 4 * (n >> 5) : 4 * (n >> 6) + 2 * (n & 1);      // 8 channels each
 #pragma unroll
                 for (int e = 0; e < kWords; ++e) *(u32x4_t*)&k_lds[stage][k_place<D>(r, piece + e)] = bf16_of_codes(x.w[e], ks).u;
+                if ((w & 1) == 0 && l == 0) gone_lds[stage][gi] = x.gone;
             } else {
                 // D = 128: chunk n / 64, keys 4q + b, 16 + 4q + b with q = n / 16 % 4, channels n % 16 + 16 (0 .. 3) of 64; D = 64: half of that
                 const int c16 = D == 128 ? n : n >> 1, ch0 = (D == 128 ? 64 * (n >> 6) : 32 * (n & 1)) + (c16 & 15), quarter = (c16 >> 4) & 3;
@@ -158,9 +153,9 @@ template <typename T, int D, int NW> __global__ __launch_bounds__(NW * 64, 1) vo
                 }
                 if ((w & 1) == 0) {
                     // a NaN must not reach rows that do not see the key (0 * NaN): the scale becomes 0, and rows that do see it are marked
-                    const bool finite = (x.extra & 0x7F80u) != 0x7F80u;
+                    const bool finite = (x.extra & 0x7F80u) != 0x7F80u || x.gone;
                     const uint32_t odd = (uint32_t)__ballot(!finite);      // lanes 32 .. 63 have the same scales
-                    if (l < 32) vs_lds[stage][32 * gi + l] = finite ? __uint_as_float(x.extra << 16) : 0.f;
+                    if (l < 32) vs_lds[stage][32 * gi + l] = finite && !x.gone ? __uint_as_float(x.extra << 16) : 0.f;
                     if (l == 0) odd_lds[stage][gi] = odd;
                 }
             }
@@ -168,7 +163,8 @@ template <typename T, int D, int NW> __global__ __launch_bounds__(NW * 64, 1) vo
     };
 
     // ---- blocks
-    auto whole = [&](int t) { return (tile0 + t) * kBN >= whole_from && (tile0 + t + 1) * kBN <= whole_to && !missing; };      // all rows of the wave see all keys
+    // tiles of whose keys all rows of the wave see all (that exist)
+    const int w0 = (whole_from + kBN - 1) / kBN - tile0, w1 = whole_to / kBN - tile0;
     // Fragments of a matrix block, in the order of its products: 4 DB of V (16 keys of 32 channels), then 2 KS of K (16 channels of 32 keys).  Each
     // is read kAhead products before it is used, the first ones (of V) in the vector block before.
     constexpr int NV = 4 * DB, NF = NV + 2 * KS, kAhead = 8;
@@ -185,11 +181,15 @@ template <typename T, int D, int NW> __global__ __launch_bounds__(NW * 64, 1) vo
         return f;
     };
     Frag fr[kAhead];
+    uint32_t odd[2] = {0, 0};
     auto read_ahead = [&](int t) {
+        odd[0] = odd_lds[t & 1][0];
+        odd[1] = odd_lds[t & 1][1];
 #pragma unroll
         for (int i = 0; i < kAhead; ++i) fr[i] = read_frag(t & 1, i);
     };
-    // probabilities of keys 16 x .. of the tile (in the order of V's pieces) times their V scales
+    // probabilities of keys 16 x .. of the tile (in the order of V's pieces) times their V scales, and their part of the row sum: here, between
+    // products, because the vector block is the longer one
     auto scaled = [&](int stage, int x, Frag (&pf)[kTerms]) {
         const float4 s0 = *(const float4*)&vs_lds[stage][8 * (2 * x + half)], s1 = *(const float4*)&vs_lds[stage][8 * (2 * x + half) + 4];
         const float a[4] = {s0.x, s0.y, s0.z, s0.w}, c[4] = {s1.x, s1.y, s1.z, s1.w};
@@ -197,6 +197,8 @@ template <typename T, int D, int NW> __global__ __launch_bounds__(NW * 64, 1) vo
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
             const float p0 = st[gi][4 * sx + e] * a[e], p1 = st[gi][8 + 4 * sx + e] * c[e];
+            sum += st[gi][4 * sx + e];
+            sum += st[gi][8 + 4 * sx + e];
             if constexpr (kTerms == 1) pf[0].u[e] = cvt_pk_bf16(p0, p1);
             else split_terms(p0, p1, [&](int term, uint32_t pair) { pf[term].u[e] = pair; });
         }
@@ -230,27 +232,24 @@ template <typename T, int D, int NW> __global__ __launch_bounds__(NW * 64, 1) vo
     };
     // a row that sees a key whose V row is NaN
     auto mark_odd = [&](int t) {
-        const uint32_t odd[2] = {odd_lds[t & 1][0], odd_lds[t & 1][1]};
         if (!__builtin_amdgcn_readfirstlane(odd[0] | odd[1])) return;
 #pragma unroll
         for (int kb = 0; kb < 2; ++kb)
             for (int r = 4 * half; r < 32; r += (r & 3) == 3 ? 5 : 1) {      // the lane's keys
                 const int key = (tile0 + t) * kBN + 32 * kb + r;
-                if ((odd[kb] >> v_slot(r) & 1u) && key >= from && key < to && !(missing && paged_group(g, b, s, key) < 0)) sum = __uint_as_float(0x7FC00000u);
+                if ((odd[kb] >> v_slot(r) & 1u) && key >= from && key < to) sum = __uint_as_float(0x7FC00000u);
             }
     };
-    auto softmax = [&](int t) {
-        const int key0 = (tile0 + t) * kBN;
-        if (!whole(t)) {
+    auto softmax = [&](int t, const uint32_t (&gone)[2]) {
+        if (t < w0 || t >= w1 || __builtin_amdgcn_readfirstlane(gone[0] | gone[1])) {
+            const int key0 = (tile0 + t) * kBN;
 #pragma unroll
-            for (int kb = 0; kb < 2; ++kb) {
-                const bool gone = missing && paged_group(g, b, s, key0 + 32 * kb) < 0;
+            for (int kb = 0; kb < 2; ++kb)
 #pragma unroll
                 for (int j = 0; j < 16; ++j) {
                     const int key = key0 + 32 * kb + 8 * (j >> 2) + 4 * half + (j & 3);
-                    if (gone || key < from || key >= to) st[kb][j] = -INFINITY;
+                    if (gone[kb] || key < from || key >= to) st[kb][j] = -INFINITY;
                 }
-            }
         }
         float mx = -INFINITY;
 #pragma unroll
@@ -272,10 +271,7 @@ template <typename T, int D, int NW> __global__ __launch_bounds__(NW * 64, 1) vo
 #pragma unroll
         for (int kb = 0; kb < 2; ++kb)
 #pragma unroll
-            for (int j = 0; j < 16; ++j) {
-                st[kb][j] = __builtin_amdgcn_exp2f(__builtin_fmaf(st[kb][j], scale, -ref));
-                sum += st[kb][j];
-            }
+            for (int j = 0; j < 16; ++j) st[kb][j] = __builtin_amdgcn_exp2f(__builtin_fmaf(st[kb][j], scale, -ref));
     };
 
     // ---- the tiles.  A wave converts set t + lead in vector block t + 1.
@@ -304,9 +300,10 @@ template <typename T, int D, int NW> __global__ __launch_bounds__(NW * 64, 1) vo
         }
         wg_barrier();      // (all that this wave has read from LDS is in the products)
         if (t + 1 < NT) {
-            if (t + 1 >= a0 && t + 1 < a1) softmax(t + 1);
+            const uint32_t gone[2] = {gone_lds[t & 1][0], gone_lds[t & 1][1]};      // (K of tile t + 1 is in set t)
             write_set(t + lead);
             load_set(t + lead + 1);
+            if (t + 1 >= a0 && t + 1 < a1) softmax(t + 1, gone);
             wait_lds_reads();      // what this wave has written is there
             if (NW == 8) read_ahead(t + 1);
         }
