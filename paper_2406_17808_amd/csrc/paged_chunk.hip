@@ -49,6 +49,7 @@ template <typename T, int D, int NW> __global__ __launch_bounds__(NW * 64, 1) vo
     constexpr int kWords = D / 32;                     // words of codes a piece has: 8 * kWords channels of a key, or 8 keys of kWords channels
     __shared__ __attribute__((aligned(16))) bf16_t k_lds[2][kBN * D], v_lds[2][kBN * D];
     __shared__ __attribute__((aligned(16))) float vs_lds[2][kBN];
+    __shared__ uint32_t special_lds;
     __shared__ uint32_t odd_lds[2][2], gone_lds[2][2];      // of a group: bits of V slots whose scale is an infinity or NaN; whether the group is missing
 
     const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), l = tid & 63, l32 = l & 31, half = l >> 5;
@@ -106,59 +107,74 @@ template <typename T, int D, int NW> __global__ __launch_bounds__(NW * 64, 1) vo
     float top = -INFINITY, sum = 0.f;
     const float scale = g.scale * 1.44269504088896341f;
 
+    // Whether anything in the range needs the careful form of a tile: a group that is missing (looked for here), a V row of NaN (seen when it is
+    // converted).  It stays set: the fast form ends for the rest.
+    bool missing = false;
+    for (int i = tid; i < 2 * NT; i += NW * 64) {
+        const int p = (2 * tile0 + i) * kGroupTokens;
+        missing |= p < to_of(pos_of(row0 + kRows - 1)) && paged_group(g, b, s, p) < 0;
+    }
+    missing = __syncthreads_or(missing);
+    if (tid == 0) special_lds = missing;
+
     // ---- codes -> LDS
-    // item i of a wave is pieces 64 (w % 2) .. of group w / 2 % 2, w = wave + NW * i; K for w < 4
+    // item i of a wave is pieces 64 (w % 2) .. of group w / 2 % 2, w = wave + NW * i; K for w < 4 (of a thread: the same piece of K and V)
+    const int n = (wave & 1) * 64 + l, gi = (wave & 3) >> 1;
+    // K, D = 128: block n / 32 of key n % 32; D = 64: half n % 2 of block n / 64 of key n / 2 % 32.  Its scale's byte stands next to that of the key 16 apart.
+    const int key = D == 128 ? n & 31 : (n >> 1) & 31, k_block = D == 128 ? n >> 5 : n >> 6;
+    const int k_to = k_place<D>(32 * gi + key, D == 128 ? 4 * k_block : 4 * k_block + 2 * (n & 1)) * 2;      // bytes; its pieces of 8 channels: XOR 16 e
+    // V, D = 128: chunk n / 64, keys 4q + b, 16 + 4q + b with q = n / 16 % 4, channels n % 16 + 16 (0 .. 3) of 64; D = 64: half of that
+    const int c16 = D == 128 ? n : n >> 1, v_to = v_place((D == 128 ? 64 * (n >> 6) : 32 * (n & 1)) + (c16 & 15), 4 * gi + ((c16 >> 4) & 3)) * 2;
     auto tile_of = [&](int item, int set) { return wave + NW * item < 4 ? set + 1 : set; };
     Piece<kWords> held[kItems];
     int numbers[kItems];      // lane l: place of the item's group in tile 64 * k + l
+    auto load_tile = [&](int i, int t) {
+        if ((t & 63) == 0) numbers[i] = t + l < NT ? (int)paged_group(g, b, s, ((tile0 + t + l) * 2 + gi) * kGroupTokens) : -1;
+        const bool is_k = wave + NW * i < 4;
+        const int at = __builtin_amdgcn_readlane(numbers[i], t & 63);
+        const uint8_t* group = g.pages + (int64_t)(max(at, 0) + hk * g.groups) * g.group_bytes;
+        held[i].load(group + (is_k ? 0 : 16 * D) + n * (4 * kWords));
+        held[i].extra = *(const uint16_t*)(group + (is_k ? 32 * D + k_block * 32 + (key & 15) * 2 : 33 * D + 2 * l32));
+        held[i].gone = at < 0;
+    };
+    auto write_codes = [&](int i, int stage) {
+        const Piece<kWords>& x = held[i];
+        if (wave + NW * i < 4) {
+            const float ks = scale_of_byte(x.extra >> (key >> 4) * 8 & 255u);
+            char* to = (char*)&k_lds[0][0] + stage * (kBN * D * 2);
+#pragma unroll
+            for (int e = 0; e < kWords; ++e) *(u32x4_t*)(to + (k_to ^ (16 * e))) = bf16_of_codes(x.w[e], ks).u;
+            return;
+        }
+        char* to = (char*)&v_lds[0][0] + stage * (kBN * D * 2) + v_to;
+#pragma unroll
+        for (int e = 0; e < kWords; e += 2) {
+            const uint32_t a = x.w[e], c = x.w[e + 1];
+            *(u32x4_t*)(to + 32 * e * kBN) = bf16_of_codes((a & 0x0F0F0F0Fu) | ((c << 4) & 0xF0F0F0F0u), 1.f).u;
+            *(u32x4_t*)(to + 32 * (e + 1) * kBN) = bf16_of_codes(((a >> 4) & 0x0F0F0F0Fu) | (c & 0xF0F0F0F0u), 1.f).u;
+        }
+        if (wave & 1) return;
+        // a NaN must not reach rows that do not see the key (0 * NaN): the scale becomes 0, and rows that do see it are marked
+        const bool finite = (x.extra & 0x7F80u) != 0x7F80u;
+        if (l < 32) vs_lds[stage][32 * gi + l] = finite && !x.gone ? __uint_as_float(x.extra << 16) : 0.f;
+        const uint32_t odd = x.gone ? 0u : (uint32_t)__ballot(!finite);      // lanes 32 .. 63 have the same scales
+        if (odd && l == 0) special_lds = 1;
+        if (l == 0) odd_lds[stage][gi] = odd;
+    };
     auto load_set = [&](int set) {
 #pragma unroll
         for (int i = 0; i < kItems; ++i) {
-            const int t = tile_of(i, set), w = wave + NW * i, gi = (w & 3) >> 1;
-            if (t < 0 || t >= NT) continue;
-            if ((t & 63) == 0) numbers[i] = t + l < NT ? (int)paged_group(g, b, s, ((tile0 + t + l) * 2 + gi) * kGroupTokens) : -1;
-            const int at = __builtin_amdgcn_readlane(numbers[i], t & 63), n = (w & 1) * 64 + l;      // piece of the group, 0 .. 127
-            const uint8_t* group = g.pages + ((int64_t)max(at, 0) + hk * g.groups) * g.group_bytes;
-            held[i].load(group + (w < 4 ? 0 : 16 * D) + n * (4 * kWords));
-            if (w < 4) held[i].extra = group[D == 128 ? k_exp_byte(D, n >> 5, n & 31) : k_exp_byte(D, n >> 6, (n >> 1) & 31)];
-            else if ((w & 1) == 0) held[i].extra = *(const uint16_t*)(group + 33 * D + 2 * l32);
-            held[i].gone = at < 0;
+            const int t = tile_of(i, set);
+            if (t >= 0 && t < NT) load_tile(i, t);
         }
     };
     auto write_set = [&](int set) {
-        const int stage = set & 1;
 #pragma unroll
         for (int i = 0; i < kItems; ++i) {
-            const int t = tile_of(i, set), w = wave + NW * i, gi = (w & 3) >> 1, n = (w & 1) * 64 + l;
+            const int t = tile_of(i, set);
             if (t < 0 || t >= NT) continue;
-            const Piece<kWords>& x = held[i];
-            if (w < 4) {
-                // D = 128: block n / 32 of key n % 32; D = 64: half n % 2 of block n / 64 of key n / 2 % 32
-                const float ks = scale_of_byte(x.extra);
-                const int r = 32 * gi + (D == 128 ? n & 31 : (n >> 1) & 31);
-                const int piece = D == 128 ? 4 * (n >> 5) : 4 * (n >> 6) + 2 * (n & 1);      // 8 channels each
-#pragma unroll
-                for (int e = 0; e < kWords; ++e) *(u32x4_t*)&k_lds[stage][k_place<D>(r, piece + e)] = bf16_of_codes(x.w[e], ks).u;
-                if ((w & 1) == 0 && l == 0) gone_lds[stage][gi] = x.gone;
-            } else {
-                // D = 128: chunk n / 64, keys 4q + b, 16 + 4q + b with q = n / 16 % 4, channels n % 16 + 16 (0 .. 3) of 64; D = 64: half of that
-                const int c16 = D == 128 ? n : n >> 1, ch0 = (D == 128 ? 64 * (n >> 6) : 32 * (n & 1)) + (c16 & 15), quarter = (c16 >> 4) & 3;
-#pragma unroll
-                for (int e = 0; e < kWords; e += 2) {
-                    const uint32_t a = x.w[e], c = x.w[e + 1];
-                    const uint32_t lo = (a & 0x0F0F0F0Fu) | ((c << 4) & 0xF0F0F0F0u), hi = ((a >> 4) & 0x0F0F0F0Fu) | (c & 0xF0F0F0F0u);
-                    const int ch = ch0 + 16 * e;
-                    *(u32x4_t*)&v_lds[stage][v_place(ch, 4 * gi + quarter)] = bf16_of_codes(lo, 1.f).u;
-                    *(u32x4_t*)&v_lds[stage][v_place(ch + 16, 4 * gi + quarter)] = bf16_of_codes(hi, 1.f).u;
-                }
-                if ((w & 1) == 0) {
-                    // a NaN must not reach rows that do not see the key (0 * NaN): the scale becomes 0, and rows that do see it are marked
-                    const bool finite = (x.extra & 0x7F80u) != 0x7F80u || x.gone;
-                    const uint32_t odd = (uint32_t)__ballot(!finite);      // lanes 32 .. 63 have the same scales
-                    if (l < 32) vs_lds[stage][32 * gi + l] = finite && !x.gone ? __uint_as_float(x.extra << 16) : 0.f;
-                    if (l == 0) odd_lds[stage][gi] = odd;
-                }
-            }
+            write_codes(i, set & 1);
+            if (wave + NW * i < 4 && !(wave & 1) && l == 0) gone_lds[set & 1][gi] = held[i].gone;
         }
     };
 
@@ -168,31 +184,33 @@ template <typename T, int D, int NW> __global__ __launch_bounds__(NW * 64, 1) vo
     // Fragments of a matrix block, in the order of its products: 4 DB of V (16 keys of 32 channels), then 2 KS of K (16 channels of 32 keys).  Each
     // is read kAhead products before it is used, the first ones (of V) in the vector block before.
     constexpr int NV = 4 * DB, NF = NV + 2 * KS, kAhead = 8;
-    const bf16_t* v_lane[4];      // V piece 2 (2 gi + sx) + half of row l32, stage 0
-    const bf16_t* k_lane[KS];
-#pragma unroll
-    for (int x = 0; x < 4; ++x) v_lane[x] = &v_lds[0][v_place(l32, 2 * x + half)];      // (rows 32 apart have the same order)
-#pragma unroll
-    for (int ks = 0; ks < KS; ++ks) k_lane[ks] = &k_lds[0][k_place<D>(l32, 2 * ks + half)];
+    // (Pieces two apart lie 32 bytes apart but for the row's XOR: one place for all.)
+    const int v_lane = v_place(l32, half) * 2, k_lane = k_place<D>(l32, half) * 2;      // bytes
     auto read_frag = [&](int stage, int i) {
         Frag f;
-        if (i < NV) f.u = *(const u32x4_t*)(v_lane[i / DB] + stage * (kBN * D) + (i % DB) * (32 * kBN));
-        else f.u = *(const u32x4_t*)(k_lane[(i - NV) >> 1] + stage * (kBN * D) + ((i - NV) & 1) * (32 * D));
+        const char* v = (const char*)&v_lds[0][0] + stage * (kBN * D * 2);
+        const char* k = (const char*)&k_lds[0][0] + stage * (kBN * D * 2);
+        if (i < NV) f.u = *(const u32x4_t*)(v + (v_lane ^ (32 * (i / DB))) + (i % DB) * (64 * kBN));      // (rows 32 apart have the same order)
+        else f.u = *(const u32x4_t*)(k + (k_lane ^ (32 * ((i - NV) >> 1))) + ((i - NV) & 1) * (64 * D));
         return f;
     };
     Frag fr[kAhead];
-    uint32_t odd[2] = {0, 0};
-    auto read_ahead = [&](int t) {
-        odd[0] = odd_lds[t & 1][0];
-        odd[1] = odd_lds[t & 1][1];
-#pragma unroll
-        for (int i = 0; i < kAhead; ++i) fr[i] = read_frag(t & 1, i);
+    float4 scales[2];      // V scales of the lane's keys 16 x .. of the tile, in the order of V's pieces
+    uint32_t special = missing;
+    auto read_scales = [&](int stage, int x) {
+        scales[0] = *(const float4*)&vs_lds[stage][8 * (2 * x + half)];
+        scales[1] = *(const float4*)&vs_lds[stage][8 * (2 * x + half) + 4];
     };
-    // probabilities of keys 16 x .. of the tile (in the order of V's pieces) times their V scales, and their part of the row sum: here, between
-    // products, because the vector block is the longer one
-    auto scaled = [&](int stage, int x, Frag (&pf)[kTerms]) {
-        const float4 s0 = *(const float4*)&vs_lds[stage][8 * (2 * x + half)], s1 = *(const float4*)&vs_lds[stage][8 * (2 * x + half) + 4];
-        const float a[4] = {s0.x, s0.y, s0.z, s0.w}, c[4] = {s1.x, s1.y, s1.z, s1.w};
+    auto read_ahead = [&](int stage) {
+        if (NW == 8) special = special_lds;
+        read_scales(stage, 0);
+#pragma unroll
+        for (int i = 0; i < kAhead; ++i) fr[i] = read_frag(stage, i);
+    };
+    // probabilities of keys 16 x .. of the tile times their V scales, and their part of the row sum: here, between products, because the vector
+    // block is the longer one
+    auto scaled = [&](int x, Frag (&pf)[kTerms]) {
+        const float a[4] = {scales[0].x, scales[0].y, scales[0].z, scales[0].w}, c[4] = {scales[1].x, scales[1].y, scales[1].z, scales[1].w};
         const int gi = x >> 1, sx = x & 1;
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
@@ -203,21 +221,23 @@ template <typename T, int D, int NW> __global__ __launch_bounds__(NW * 64, 1) vo
             else split_terms(p0, p1, [&](int term, uint32_t pair) { pf[term].u[e] = pair; });
         }
     };
-    // P V of tile t (its first fragments are in fr), K Q^T of tile t + 1.  One form for all tiles: before a wave's first tile the probabilities are 0
-    // and V finite, behind its last nobody looks at the logits.  (Forms without the one or the other cost copies of all outputs where they meet.)
-    auto matrix_block = [&](int t) {
-        const int stage = t & 1;
+    // P V of tile t (its first fragments and scales are there), K Q^T of tile t + 1, from the stage of set t.  One form for all tiles: before a wave's
+    // first tile the probabilities are 0 and V finite, behind its last nobody looks at the logits.  (Forms without the one or the other cost
+    // copies of all outputs where they meet.)  Scales are asked for three products before they are used: LDS answers in order, so a wait for
+    // them is a wait for all fragments asked for before.
+    auto matrix_block = [&](int stage) {
         Frag pf[2][kTerms];
-        scaled(stage, 0, pf[0]);
+        scaled(0, pf[0]);
         __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
         for (int i = 0; i < NF; ++i) {
             const Frag f = fr[i % kAhead];
             if (i < NV) {
                 const int x = i / DB;
+                if (i % DB == 0 && x < 3) read_scales(stage, x + 1);
 #pragma unroll
                 for (int y = 0; y < kTerms; ++y) o[i % DB] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(f.v, pf[x & 1][y].v, o[i % DB], 0, 0, 0);
-                if (i % DB == 0 && x < 3) scaled(stage, x + 1, pf[(x + 1) & 1]);
+                if (i % DB == DB - 1 && x < 3) scaled(x + 1, pf[(x + 1) & 1]);
             } else {
                 const int ks = (i - NV) >> 1, kb = (i - NV) & 1;
                 if (ks == 0)
@@ -232,6 +252,7 @@ template <typename T, int D, int NW> __global__ __launch_bounds__(NW * 64, 1) vo
     };
     // a row that sees a key whose V row is NaN
     auto mark_odd = [&](int t) {
+        const uint32_t odd[2] = {odd_lds[t & 1][0], odd_lds[t & 1][1]};
         if (!__builtin_amdgcn_readfirstlane(odd[0] | odd[1])) return;
 #pragma unroll
         for (int kb = 0; kb < 2; ++kb)
@@ -240,17 +261,19 @@ template <typename T, int D, int NW> __global__ __launch_bounds__(NW * 64, 1) vo
                 if ((odd[kb] >> v_slot(r) & 1u) && key >= from && key < to) sum = __uint_as_float(0x7FC00000u);
             }
     };
-    auto softmax = [&](int t, const uint32_t (&gone)[2]) {
-        if (t < w0 || t >= w1 || __builtin_amdgcn_readfirstlane(gone[0] | gone[1])) {
-            const int key0 = (tile0 + t) * kBN;
+    auto mask = [&](int t) {      // what a row does not see
+        const uint32_t gone[2] = {gone_lds[(t + 1) & 1][0], gone_lds[(t + 1) & 1][1]};      // (K of tile t is in set t - 1)
+        if (t >= w0 && t < w1 && !__builtin_amdgcn_readfirstlane(gone[0] | gone[1])) return;
+        const int key0 = (tile0 + t) * kBN;
 #pragma unroll
-            for (int kb = 0; kb < 2; ++kb)
+        for (int kb = 0; kb < 2; ++kb)
 #pragma unroll
-                for (int j = 0; j < 16; ++j) {
-                    const int key = key0 + 32 * kb + 8 * (j >> 2) + 4 * half + (j & 3);
-                    if (gone[kb] || key < from || key >= to) st[kb][j] = -INFINITY;
-                }
-        }
+            for (int j = 0; j < 16; ++j) {
+                const int key = key0 + 32 * kb + 8 * (j >> 2) + 4 * half + (j & 3);
+                if (gone[kb] || key < from || key >= to) st[kb][j] = -INFINITY;
+            }
+    };
+    auto softmax = [&]() {
         float mx = -INFINITY;
 #pragma unroll
         for (int kb = 0; kb < 2; ++kb)
@@ -279,6 +302,8 @@ template <typename T, int D, int NW> __global__ __launch_bounds__(NW * 64, 1) vo
     for (int i = tid; i < kBN * D / 8; i += NW * 64) *(u32x4_t*)&v_lds[1][8 * i] = u32x4_t{0, 0, 0, 0};      // matrix block -1 multiplies them with 0
     if (tid < kBN) vs_lds[1][tid] = 0.f;
     if (tid < 2) odd_lds[1][tid] = 0;
+    wait_lds_reads();
+    wg_barrier();      // (special_lds as well: a wave that converts may set it)
     for (int set = -1; set < lead - 1; ++set) {
         load_set(set);
         write_set(set);
@@ -289,24 +314,36 @@ template <typename T, int D, int NW> __global__ __launch_bounds__(NW * 64, 1) vo
     wait_lds_reads();
     wg_barrier();
     if (late) wg_barrier();
-    if (NW == 8 && a0 == 0) read_ahead(-1);
+    if (NW == 8 && a0 == 0) read_ahead(1);
+    // Tiles of whose successor all rows of the wave see all keys, with tile t + 3 there: nothing to test but whether something special came up.  (A wave
+    // issues an instruction every five to six cycles whatever it is, and the vector block is the longer one.)
+    const int plain0 = max(max(a0, w0) - 1, 0), plain1 = min(min(a1, w1) - 1, NT - 3);
     for (int t = -1; t < NT; ++t) {
-        if (t >= a0 - 1 && t < a1) {
-            if (NW == 4) read_ahead(t);      // (V of the tile is written in the vector block before)
-            mark_odd(t);
+        if (NW == 4) special = special_lds;
+        const bool plain = t >= plain0 && t < plain1 && !__builtin_amdgcn_readfirstlane(special);
+        if (plain || (t >= a0 - 1 && t < a1)) {
+            if (NW == 4) read_ahead(t & 1);      // (V of the tile is written in the vector block before)
+            if (!plain) mark_odd(t);
             __builtin_amdgcn_s_setprio(1);
-            matrix_block(t);
+            matrix_block(t & 1);
             __builtin_amdgcn_s_setprio(0);
         }
         wg_barrier();      // (all that this wave has read from LDS is in the products)
-        if (t + 1 < NT) {
-            const uint32_t gone[2] = {gone_lds[t & 1][0], gone_lds[t & 1][1]};      // (K of tile t + 1 is in set t)
+        if (plain) {
+#pragma unroll
+            for (int i = 0; i < kItems; ++i) {
+                write_codes(i, (t + lead) & 1);
+                load_tile(i, tile_of(i, t + lead + 1));
+            }
+        } else if (t + 1 < NT) {
             write_set(t + lead);
             load_set(t + lead + 1);
-            if (t + 1 >= a0 && t + 1 < a1) softmax(t + 1, gone);
-            wait_lds_reads();      // what this wave has written is there
-            if (NW == 8) read_ahead(t + 1);
         }
+        const bool seen = t + 1 >= a0 && t + 1 < a1;
+        if (!plain && seen) mask(t + 1);
+        if (plain || seen) softmax();
+        wait_lds_reads();      // what this wave has written is there
+        if (NW == 8) read_ahead((t + 1) & 1);
         wg_barrier();
     }
     if (!late && NW == 8) wg_barrier();
