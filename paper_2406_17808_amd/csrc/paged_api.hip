@@ -79,8 +79,8 @@ static int check_paged_config(const cascade_paged_config* c, PagedGeom& g)
     g.page_size = c->page_size;
     g.groups = c->page_size / kGroupTokens;
     g.group_bytes = paged_group_bytes(g.d);
-    // page numbers are 32-bit, and 2^47 bytes are more than any device can address
-    if (c->n_pages < 1 || c->n_pages > 0x7FFFFFFF || c->n_pages > (1ll << 47) / ((int64_t)g.Hkv * g.groups * g.group_bytes))
+    // page numbers are 32-bit, places of groups in units of 128 bytes as well: 2^39 bytes, more than a device has
+    if (c->n_pages < 1 || c->n_pages > 0x7FFFFFFF || c->n_pages > (1ll << 39) / ((int64_t)g.Hkv * g.groups * g.group_bytes))
         return fail(nullptr, CASCADE_E_INVALID_CONFIG, "%s: n_pages out of range", who);
     g.n_pages = c->n_pages;
     g.scale = c->softmax_scale == 0.f ? 1.f / sqrtf((float)g.d) : c->softmax_scale;

@@ -112,7 +112,7 @@ template <typename T, int D, int NW> __global__ __launch_bounds__(NW * 64, 1) vo
     bool missing = false;
     for (int i = tid; i < 2 * NT; i += NW * 64) {
         const int p = (2 * tile0 + i) * kGroupTokens;
-        missing |= p < to_of(pos_of(row0 + kRows - 1)) && paged_group(g, b, s, p) < 0;
+        missing |= p < to_of(pos_of(row0 + kRows - 1)) && p + kGroupTokens > from_of(pos_of(row0)) && paged_group(g, b, s, p) < 0;
     }
     missing = __syncthreads_or(missing);
     if (tid == 0) special_lds = missing;
@@ -127,17 +127,24 @@ template <typename T, int D, int NW> __global__ __launch_bounds__(NW * 64, 1) vo
     const int c16 = D == 128 ? n : n >> 1, v_to = v_place((D == 128 ? 64 * (n >> 6) : 32 * (n & 1)) + (c16 & 15), 4 * gi + ((c16 >> 4) & 3)) * 2;
     auto tile_of = [&](int item, int set) { return wave + NW * item < 4 ? set + 1 : set; };
     Piece<kWords> held[kItems];
-    int numbers[kItems];      // lane l: place of the item's group in tile 64 * k + l
-    auto load_tile = [&](int i, int t) {
-        if ((t & 63) == 0) numbers[i] = t + l < NT ? (int)paged_group(g, b, s, ((tile0 + t + l) * 2 + gi) * kGroupTokens) : -1;
+    // lane l: place of the item's group in tile 64 * k + l, in units of 128 bytes; ~0: the group is missing
+    uint32_t places[kItems];
+    constexpr uint32_t kGroupUnits = paged_group_bytes(D) / 128;
+    const uint32_t last_place = (uint32_t)(g.n_pages * g.Hkv * g.groups - 1) * kGroupUnits;
+    auto load_tile = [&](int i, int t, auto plain) {
+        if (__builtin_expect((t & 63) == 0, 0)) {
+            const int64_t at = t + l < NT ? paged_group(g, b, s, ((tile0 + t + l) * 2 + gi) * kGroupTokens) : -1;
+            places[i] = at < 0 ? ~0u : (uint32_t)(at + (int64_t)hk * g.groups) * kGroupUnits;
+        }
         const bool is_k = wave + NW * i < 4;
-        const int at = __builtin_amdgcn_readlane(numbers[i], t & 63);
-        const uint8_t* group = g.pages + (int64_t)(max(at, 0) + hk * g.groups) * g.group_bytes;
+        uint32_t at = __builtin_amdgcn_readlane(places[i], t & 63);
+        held[i].gone = !decltype(plain)::value && at == ~0u;
+        at = min(at, last_place);      // a group that is missing: any other's bytes, which nobody sees
+        const uint8_t* group = g.pages + ((uint64_t)at << 7);
         held[i].load(group + (is_k ? 0 : 16 * D) + n * (4 * kWords));
         held[i].extra = *(const uint16_t*)(group + (is_k ? 32 * D + k_block * 32 + (key & 15) * 2 : 33 * D + 2 * l32));
-        held[i].gone = at < 0;
     };
-    auto write_codes = [&](int i, int stage) {
+    auto write_codes = [&](int i, int stage, auto plain) {
         const Piece<kWords>& x = held[i];
         if (wave + NW * i < 4) {
             const float ks = scale_of_byte(x.extra >> (key >> 4) * 8 & 255u);
@@ -156,16 +163,16 @@ template <typename T, int D, int NW> __global__ __launch_bounds__(NW * 64, 1) vo
         if (wave & 1) return;
         // a NaN must not reach rows that do not see the key (0 * NaN): the scale becomes 0, and rows that do see it are marked
         const bool finite = (x.extra & 0x7F80u) != 0x7F80u;
-        if (l < 32) vs_lds[stage][32 * gi + l] = finite && !x.gone ? __uint_as_float(x.extra << 16) : 0.f;
+        vs_lds[stage][32 * gi + l32] = finite && !x.gone ? __uint_as_float(x.extra << 16) : 0.f;
         const uint32_t odd = x.gone ? 0u : (uint32_t)__ballot(!finite);      // lanes 32 .. 63 have the same scales
-        if (odd && l == 0) special_lds = 1;
-        if (l == 0) odd_lds[stage][gi] = odd;
+        if (__builtin_expect(odd != 0u, 0)) special_lds = 1;
+        if (!decltype(plain)::value || __builtin_expect(odd != 0u, 0)) odd_lds[stage][gi] = odd;      // (0 as long as nothing was special)
     };
     auto load_set = [&](int set) {
 #pragma unroll
         for (int i = 0; i < kItems; ++i) {
             const int t = tile_of(i, set);
-            if (t >= 0 && t < NT) load_tile(i, t);
+            if (t >= 0 && t < NT) load_tile(i, t, std::false_type());
         }
     };
     auto write_set = [&](int set) {
@@ -173,7 +180,7 @@ template <typename T, int D, int NW> __global__ __launch_bounds__(NW * 64, 1) vo
         for (int i = 0; i < kItems; ++i) {
             const int t = tile_of(i, set);
             if (t < 0 || t >= NT) continue;
-            write_codes(i, set & 1);
+            write_codes(i, set & 1, std::false_type());
             if (wave + NW * i < 4 && !(wave & 1) && l == 0) gone_lds[set & 1][gi] = held[i].gone;
         }
     };
@@ -183,7 +190,7 @@ template <typename T, int D, int NW> __global__ __launch_bounds__(NW * 64, 1) vo
     const int w0 = (whole_from + kBN - 1) / kBN - tile0, w1 = whole_to / kBN - tile0;
     // Fragments of a matrix block, in the order of its products: 4 DB of V (16 keys of 32 channels), then 2 KS of K (16 channels of 32 keys).  Each
     // is read kAhead products before it is used, the first ones (of V) in the vector block before.
-    constexpr int NV = 4 * DB, NF = NV + 2 * KS, kAhead = 8;
+    constexpr int NV = 4 * DB, NF = NV + 2 * KS, kAhead = 6;
     // (Pieces two apart lie 32 bytes apart but for the row's XOR: one place for all.)
     const int v_lane = v_place(l32, half) * 2, k_lane = k_place<D>(l32, half) * 2;      // bytes
     auto read_frag = [&](int stage, int i) {
@@ -226,8 +233,8 @@ template <typename T, int D, int NW> __global__ __launch_bounds__(NW * 64, 1) vo
     // copies of all outputs where they meet.)  Scales are asked for three products before they are used: LDS answers in order, so a wait for
     // them is a wait for all fragments asked for before.
     auto matrix_block = [&](int stage) {
-        Frag pf[2][kTerms];
-        scaled(0, pf[0]);
+        Frag pf[kTerms];
+        scaled(0, pf);
         __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
         for (int i = 0; i < NF; ++i) {
@@ -236,8 +243,8 @@ template <typename T, int D, int NW> __global__ __launch_bounds__(NW * 64, 1) vo
                 const int x = i / DB;
                 if (i % DB == 0 && x < 3) read_scales(stage, x + 1);
 #pragma unroll
-                for (int y = 0; y < kTerms; ++y) o[i % DB] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(f.v, pf[x & 1][y].v, o[i % DB], 0, 0, 0);
-                if (i % DB == DB - 1 && x < 3) scaled(x + 1, pf[(x + 1) & 1]);
+                for (int y = 0; y < kTerms; ++y) o[i % DB] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(f.v, pf[y].v, o[i % DB], 0, 0, 0);
+                if (i % DB == DB - 1 && x < 3) scaled(x + 1, pf);
             } else {
                 const int ks = (i - NV) >> 1, kb = (i - NV) & 1;
                 if (ks == 0)
@@ -315,35 +322,44 @@ template <typename T, int D, int NW> __global__ __launch_bounds__(NW * 64, 1) vo
     wg_barrier();
     if (late) wg_barrier();
     if (NW == 8 && a0 == 0) read_ahead(1);
-    // Tiles of whose successor all rows of the wave see all keys, with tile t + 3 there: nothing to test but whether something special came up.  (A wave
+    // Tiles of whose successor all rows of the wave see all keys, with all keys of tile t + 3 there (the last tile may end in a group that does not exist): nothing
+    // to test but whether something special came up.  (A wave
     // issues an instruction every five to six cycles whatever it is, and the vector block is the longer one.)
-    const int plain0 = max(max(a0, w0) - 1, 0), plain1 = min(min(a1, w1) - 1, NT - 3);
-    for (int t = -1; t < NT; ++t) {
-        if (NW == 4) special = special_lds;
-        const bool plain = t >= plain0 && t < plain1 && !__builtin_amdgcn_readfirstlane(special);
-        if (plain || (t >= a0 - 1 && t < a1)) {
+    const int plain0 = max(max(a0, w0) - 1, 0), plain1 = min(min(a1, w1) - 1, NT - 4);
+    int t = -1;
+    while (t < NT) {
+        if (NW == 8 && t >= plain0 && t < plain1 && !__builtin_amdgcn_readfirstlane(special)) {
+            do {
+                __builtin_amdgcn_s_setprio(1);
+                matrix_block(t & 1);
+                __builtin_amdgcn_s_setprio(0);
+                wg_barrier();
+                write_codes(0, (t + lead) & 1, std::true_type());
+                load_tile(0, t + 3, std::true_type());
+                softmax();
+                wait_lds_reads();
+                ++t;
+                read_ahead(t & 1);
+                wg_barrier();
+            } while (t < plain1 && !__builtin_amdgcn_readfirstlane(special));
+        }
+        if (t >= a0 - 1 && t < a1) {
             if (NW == 4) read_ahead(t & 1);      // (V of the tile is written in the vector block before)
-            if (!plain) mark_odd(t);
-            __builtin_amdgcn_s_setprio(1);
+            mark_odd(t);
             matrix_block(t & 1);
-            __builtin_amdgcn_s_setprio(0);
         }
         wg_barrier();      // (all that this wave has read from LDS is in the products)
-        if (plain) {
-#pragma unroll
-            for (int i = 0; i < kItems; ++i) {
-                write_codes(i, (t + lead) & 1);
-                load_tile(i, tile_of(i, t + lead + 1));
-            }
-        } else if (t + 1 < NT) {
+        if (t + 1 < NT) {
             write_set(t + lead);
             load_set(t + lead + 1);
         }
-        const bool seen = t + 1 >= a0 && t + 1 < a1;
-        if (!plain && seen) mask(t + 1);
-        if (plain || seen) softmax();
+        if (t + 1 >= a0 && t + 1 < a1) {
+            mask(t + 1);
+            softmax();
+        }
         wait_lds_reads();      // what this wave has written is there
-        if (NW == 8) read_ahead((t + 1) & 1);
+        ++t;
+        if (NW == 8) read_ahead(t & 1);
         wg_barrier();
     }
     if (!late && NW == 8) wg_barrier();
