@@ -9,17 +9,16 @@ namespace ckv {
 typedef __attribute__((ext_vector_type(4))) float f32x4_t;
 
 constexpr int kFewWaves = 4;        // waves of a workgroup for few rows
-constexpr int kFewRows = 32;        // rows of a sequence and KV head that it takes
-constexpr int kFewParts = 4096;     // most partial results of a launch (sequences x KV heads x splits), of kFewRows rows each
-
+constexpr int kFewRows = 32, kFewMostRows = 512;      // rows of a sequence and KV head that it takes: always, and where it is the cheaper one
 constexpr int kFewMaxSplits = 512;
 
 struct FewPlan {
     int groups_per_split, splits;
     int max_rows;      // rows of a sequence and KV head: more are left to the other kernel
+    int block_rows;    // rows of a workgroup: 16 or 32
 };
 
-constexpr int kChunkPartRows = 512 * 256;      // rows of partial results that a split launch for many rows may have
+constexpr int kChunkPartRows = 512 * 256;      // rows of partial results that a split launch may have
 
 struct ChunkPlan {
     int units;         // at least the row blocks of all sequences
@@ -38,14 +37,14 @@ __device__ inline bool find_row_block(const PagedGeom& g, const PagedBatch& b, c
     }, unit, seq, block);
 }
 
-// Groups of 32 keys that some new token of a sequence sees: [first, last)
+// Groups of 32 keys that the new tokens i0 .. i1 of a sequence see: [first, last)
 struct KeySpan {
     int first, last;
 };
-__device__ inline KeySpan key_span(const PagedGeom& g, const PagedBatch& b, const SeqView& v)
+__device__ inline KeySpan key_span(const PagedGeom& g, const PagedBatch& b, const SeqView& v, int i0, int i1)
 {
     KeySpan k;
-    const int from = g.window && v.len >= g.window ? v.len - g.window + 1 : 0, to = min(v.len + v.n, b.max_length);
+    const int from = g.window && v.len + i0 >= g.window ? v.len + i0 - g.window + 1 : 0, to = min(v.len + i1 + 1, b.max_length);
     k.first = from / kGroupTokens;
     k.last = max(k.first, (to + kGroupTokens - 1) / kGroupTokens);
     return k;

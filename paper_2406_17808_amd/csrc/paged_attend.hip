@@ -7,7 +7,7 @@
 namespace ckv {
 
 // ------------------------------------------------------------------ few rows
-// out = softmax(scale Q K^T) V for at most 16 * NT rows (new tokens x query heads of one KV head), bound by the bytes of the cache.
+// out = softmax(scale Q K^T) V for blocks of 16 * NT rows (new tokens x query heads of one KV head), bound by the bytes of the cache.
 //
 // v_mfma_f32_16x16x32_bf16: S^T = K Q^T, keys are rows and queries columns.  A lane (m = l % 16, q = l / 16) takes key m of 16
 // and a quarter of the channels, D/4 consecutive ones: one 16-byte piece of codes (D = 128) with one scale, turned into bf16 by
@@ -93,20 +93,21 @@ template <typename T, int D, int NT> __global__ __launch_bounds__(kFewWaves * 64
     static_assert(sizeof(WaveRows) <= kFewStages * kStage, "outputs fit the stages");
     WaveRows* o_wave = (WaveRows*)ring;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), m = lane & 15, qq = lane >> 4;
-    const int split = blockIdx.x, hk = blockIdx.y, s = blockIdx.z;
+    const int split = blockIdx.x, hk = blockIdx.y % g.Hkv, row0 = blockIdx.y / g.Hkv * (16 * NT), s = blockIdx.z;
     const SeqView v = seq_view(b, s);
     const int rows = v.n * g.G;
-    if (rows == 0 || rows > plan.max_rows) return;
-    const KeySpan span = key_span(g, b, v);
+    if (row0 >= rows || rows > plan.max_rows) return;
+    const int i0 = row0 / g.G, i1 = (min(row0 + 16 * NT, rows) - 1) / g.G;      // the block's tokens
+    const KeySpan span = key_span(g, b, v, i0, i1);
     const int per = plan.groups_per_split, first = span.first + split * per, last = min(first + per, span.last);
     if (split > 0 && first >= span.last) return;      // split 0 also stands for a sequence that sees nothing
 
     // queries: column m + 16 n, the channels that this lane's keys have
     Frag qf[NT][kTerms][kSteps];
-    int pos[NT];      // of the column's token; columns without a row stand for row 0
+    int pos[NT];      // of the column's token; columns without a row stand for the block's first
 #pragma unroll
     for (int n = 0; n < NT; ++n) {
-        const int c = m + 16 * n, i = c < rows ? c / g.G : 0, h = c < rows ? c - i * g.G : 0;
+        const int row = row0 + m + 16 * n < rows ? row0 + m + 16 * n : row0, i = row / g.G, h = row - i * g.G;
         pos[n] = v.len + i;
         const T* x = q + (v.first + i) * q_stride + (hk * g.G + h) * D + D / 4 * qq;
 #pragma unroll
@@ -134,7 +135,7 @@ template <typename T, int D, int NT> __global__ __launch_bounds__(kFewWaves * 64
     }
     const float scale = g.scale * 1.44269504088896341f;
     // groups that every column sees whole
-    const int whole_from = g.window ? v.len + v.n - g.window : 0, whole_to = min(v.len + 1, b.max_length);
+    const int whole_from = g.window ? v.len + i1 + 1 - g.window : 0, whole_to = min(v.len + i0 + 1, b.max_length);
 
     const int count = (last - first - wave + kFewWaves - 1) / kFewWaves;      // groups of this wave
     int numbers = -1;      // lane l: place of the wave's group 64 * k + l
@@ -254,7 +255,7 @@ template <typename T, int D, int NT> __global__ __launch_bounds__(kFewWaves * 64
         for (int t = 0; t < D / 16; ++t) *(f32x4_t*)&o_wave[wave][m][16 * t + 4 * qq] = o[n][t];
         __syncthreads();
         constexpr int kEach = D / 16;
-        const int c = threadIdx.x / 16, at = threadIdx.x % 16 * kEach, row = c + 16 * n;
+        const int c = threadIdx.x / 16, at = threadIdx.x % 16 * kEach, row = row0 + c + 16 * n;
         if (row < rows) {
             float all = m_wave[0][c];
 #pragma unroll
@@ -294,7 +295,8 @@ template <typename T, int D> __global__ __launch_bounds__(256) void merge_few_ke
     const int row = blockIdx.x, hk = blockIdx.y, s = blockIdx.z, tid = threadIdx.x;
     const SeqView v = seq_view(b, s);
     if (row >= v.n * g.G || v.n * g.G > plan.max_rows) return;
-    const KeySpan span = key_span(g, b, v);
+    const int row0 = row / plan.block_rows * plan.block_rows;
+    const KeySpan span = key_span(g, b, v, row0 / g.G, (min(row0 + plan.block_rows, v.n * g.G) - 1) / g.G);
     const int splits = (span.last - span.first + plan.groups_per_split - 1) / plan.groups_per_split;
     if (splits <= 1) return;      // written by its only split
     const float* x = part + ((int64_t)(s * g.Hkv + hk) * plan.splits * plan.max_rows + row) * (D + 2);
@@ -347,47 +349,69 @@ template <typename T, int D> __global__ __launch_bounds__(256) void merge_few_ke
 }
 
 // ------------------------------------------------------------------ launches
+// The longest range of keys of a batch's sequences.
+static int64_t longest_span(const PagedGeom& g, const PagedBatch& b)
+{
+    return g.window && g.window < b.max_length - b.max_new ? (int64_t)g.window + b.max_new : b.max_length;
+}
+
+// Rows of a sequence and KV head up to which the kernel for few rows takes it: kFewRows, or kFewMostRows where no sequence has more and it is the cheaper one.
+// It goes over the keys again for every 32 rows, 0.36 us for a group of keys on one compute unit; the other kernel takes 3.6 us for 64 keys and up to 256 rows (there is
+// little to overlap in a short range), and 28 us however little there is to do, 8 us here.  bf16, d 128, 8 KV heads, 16000 keys, us here and there: 64
+// rows of four sequences 52, 135; 128 rows of one 35, 58; 256 rows 49, 63; 512 rows 103, 80.  fp32 has three times the products in both and half the rows there.
+static int few_rows(const PagedGeom& g, const PagedBatch& b, int dtype)
+{
+    const int64_t most = (int64_t)b.max_new * g.G, rows = ((int64_t)b.n_tokens * g.G + b.n_seqs - 1) / b.n_seqs;      // of a sequence: the most, the mean
+    if (most <= kFewRows || most > kFewMostRows) return kFewRows;
+    const int tile = dtype == CASCADE_F32 ? 128 : 256;
+    const double work = (dtype == CASCADE_F32 ? 3.0 : 1.0) * g.d / 128 * ((double)b.n_seqs * g.Hkv / 256) * longest_span(g, b);
+    return 8 + 0.36 * work * ((rows + 31) / 32) / kGroupTokens <= 28 + 3.6 * work * ((rows + tile - 1) / tile) / 64 ? kFewMostRows : kFewRows;
+}
+
 // Splits of a launch for few rows: a share is a whole number of rounds of the workgroup's waves.  A compute unit runs three workgroups (registers; four at D =
 // 64), so that many times 256 a launch, or as many times that as leave a workgroup at most 24 rounds (sequences of different lengths even out over them: 32
 // of up to 16384 keys take 61 us, with 48 rounds 90, with 12 77).
 constexpr int kFewRounds = 24;
-static FewPlan few_plan(const PagedGeom& g, const PagedBatch& b)
+static FewPlan few_plan(const PagedGeom& g, const PagedBatch& b, int dtype)
 {
     FewPlan p;
-    const int64_t pairs = (int64_t)b.n_seqs * g.Hkv;
-    const int longest = g.window && g.window < b.max_length - b.max_new ? g.window + b.max_new + 31 : b.max_length;
-    const int64_t rounds = (longest / kGroupTokens + kFewWaves) / kFewWaves;      // of the longest sequence
-    const int64_t fill = g.d == 64 ? 1024 : 768;
-    int64_t splits = fill / pairs < 1 ? 1 : fill / pairs;
-    for (int64_t k = 2; (rounds + splits - 1) / splits > kFewRounds && fill * k / pairs * pairs <= kFewParts; ++k) splits = fill * k / pairs < 1 ? 1 : fill * k / pairs;
+    const int64_t rows = (int64_t)b.max_new * g.G;
+    const int limit = few_rows(g, b, dtype);
+    p.max_rows = rows < limit ? (int)rows : limit;
+    p.block_rows = p.max_rows <= 16 ? 16 : 32;
+    const int64_t pairs = (int64_t)b.n_seqs * g.Hkv, blocks = pairs * ((p.max_rows + p.block_rows - 1) / p.block_rows);
+    const int64_t rounds = (longest_span(g, b) / kGroupTokens + 2 + kFewWaves - 1) / kFewWaves;      // of the longest sequence (its first and last group may be begun)
+    const int64_t fill = g.d == 64 ? 1024 : 768, most = kChunkPartRows / (pairs * p.max_rows);      // (the partial results have to fit)
+    int64_t splits = fill / blocks;
+    for (int64_t k = 2; splits < most && rounds > kFewRounds * (splits < 1 ? 1 : splits) && k <= 64; ++k) splits = fill * k / blocks;
+    if (splits > most) splits = most;
     if (splits > rounds) splits = rounds;
     if (splits > kFewMaxSplits) splits = kFewMaxSplits;
+    // (the join costs 3 us and another for every 1024 rows, a round about 1: 24 new tokens of 4 heads each on 300 keys, 16 sequences, 38 us with two splits, 12 without)
+    if (splits < 1 || rounds - rounds / splits < 3 + pairs * p.max_rows / 1024) splits = 1;
     const int64_t each = (rounds + splits - 1) / splits;
     p.groups_per_split = (int)(each * kFewWaves);
     p.splits = (int)((rounds + each - 1) / each);
-    const int rows = b.max_new * g.G;
-    p.max_rows = rows < kFewRows ? rows : kFewRows;
     return p;
 }
 
-static_assert(kFewParts * kFewRows <= kChunkPartRows, "one scratch for both");
 size_t paged_scratch_bytes(const PagedGeom& g) { return (size_t)kChunkPartRows * (g.d + 2) * 4; }
 
 void launch_paged_attend(const PagedGeom& g, const PagedBatch& b, const void* q, int64_t q_stride, void* out, void* scratch, int dtype, hipStream_t s)
 {
-    const FewPlan p = few_plan(g, b);
+    const FewPlan p = few_plan(g, b, dtype);
     const int64_t rows = (int64_t)b.max_new * g.G;
     with_paged_form(dtype, g.d, [&](auto f) {
         typedef typename decltype(f)::Elt T;
         constexpr int D = decltype(f)::d;
-        const dim3 grid(p.splits, g.Hkv, b.n_seqs);
-        if (p.max_rows <= 16)
+        const dim3 grid(p.splits, g.Hkv * ((p.max_rows + p.block_rows - 1) / p.block_rows), b.n_seqs);
+        if (p.block_rows == 16)
             hipLaunchKernelGGL((attend_few_kernel<T, D, 1>), grid, dim3(kFewWaves * 64), 0, s, g, b, p, (const T*)q, q_stride, (T*)out, (float*)scratch);
         else
             hipLaunchKernelGGL((attend_few_kernel<T, D, 2>), grid, dim3(kFewWaves * 64), 0, s, g, b, p, (const T*)q, q_stride, (T*)out, (float*)scratch);
         if (p.splits > 1)
             hipLaunchKernelGGL((merge_few_kernel<T, D>), dim3(p.max_rows, g.Hkv, b.n_seqs), dim3(256), 0, s, g, b, p, (const float*)scratch, (T*)out);
-        if (rows > kFewRows)
+        if (rows > p.max_rows)
             launch_attend_chunk(g, b, p.max_rows, q, q_stride, out, scratch, dtype, s);
     });
 }
