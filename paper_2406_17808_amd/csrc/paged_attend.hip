@@ -363,8 +363,11 @@ static int few_rows(const PagedGeom& g, const PagedBatch& b, int dtype)
 {
     const int64_t most = (int64_t)b.max_new * g.G, rows = ((int64_t)b.n_tokens * g.G + b.n_seqs - 1) / b.n_seqs;      // of a sequence: the most, the mean
     if (most <= kFewRows || most > kFewMostRows) return kFewRows;
+    // (a workgroup per 32 of the most rows: not where nearly all of them would be empty, nor more than a launch can have)
+    const int64_t pair_count = (int64_t)b.n_seqs * g.Hkv, blocks = pair_count * ((most + 31) / 32);
+    if (blocks > 4096 + 2 * pair_count * ((rows + 31) / 32) || blocks > (1 << 23)) return kFewRows;
     const int tile = dtype == CASCADE_F32 ? 128 : 256;
-    const double work = (dtype == CASCADE_F32 ? 3.0 : 1.0) * g.d / 128 * ((double)b.n_seqs * g.Hkv / 256) * longest_span(g, b);
+    const double work = (dtype == CASCADE_F32 ? 3.0 : 1.0) * g.d / 128 * (pair_count / 256.0) * longest_span(g, b);
     return 8 + 0.36 * work * ((rows + 31) / 32) / kGroupTokens <= 28 + 3.6 * work * ((rows + tile - 1) / tile) / 64 ? kFewMostRows : kFewRows;
 }
 
