@@ -9,7 +9,7 @@ namespace ckv {
 typedef __attribute__((ext_vector_type(4))) float f32x4_t;
 
 constexpr int kFewWaves = 4;        // waves of a workgroup for few rows
-constexpr int kFewRows = 32, kFewMostRows = 512;      // rows of a sequence and KV head that it takes: always, and where it is the cheaper one
+constexpr int kFewRows = 32;        // rows of a sequence and KV head that it takes in any case
 constexpr int kFewMaxSplits = 512;
 
 struct FewPlan {

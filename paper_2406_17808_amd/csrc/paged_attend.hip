@@ -93,7 +93,7 @@ template <typename T, int D, int NT> __global__ __launch_bounds__(kFewWaves * 64
     static_assert(sizeof(WaveRows) <= kFewStages * kStage, "outputs fit the stages");
     WaveRows* o_wave = (WaveRows*)ring;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), m = lane & 15, qq = lane >> 4;
-    const int split = blockIdx.x, hk = blockIdx.y % g.Hkv, row0 = blockIdx.y / g.Hkv * (16 * NT), s = blockIdx.z;
+    const int split = blockIdx.x, hk = blockIdx.y % g.Hkv, row0 = (gridDim.y - 1 - blockIdx.y) / g.Hkv * (16 * NT), s = blockIdx.z;
     const SeqView v = seq_view(b, s);
     const int rows = v.n * g.G;
     if (row0 >= rows || rows > plan.max_rows) return;
@@ -355,31 +355,15 @@ static int64_t longest_span(const PagedGeom& g, const PagedBatch& b)
     return g.window && g.window < b.max_length - b.max_new ? (int64_t)g.window + b.max_new : b.max_length;
 }
 
-// Rows of a sequence and KV head up to which the kernel for few rows takes it: kFewRows, or kFewMostRows where no sequence has more and it is the cheaper one.
-// It goes over the keys again for every 32 rows, 0.36 us for a group of keys on one compute unit; the other kernel takes 3.6 us for 64 keys and up to 256 rows (there is
-// little to overlap in a short range), and 28 us however little there is to do, 8 us here.  bf16, d 128, 8 KV heads, 16000 keys, us here and there: 64
-// rows of four sequences 52, 135; 128 rows of one 35, 58; 256 rows 49, 63; 512 rows 103, 80.  fp32 has three times the products in both and half the rows there.
-static int few_rows(const PagedGeom& g, const PagedBatch& b, int dtype)
-{
-    const int64_t most = (int64_t)b.max_new * g.G, rows = ((int64_t)b.n_tokens * g.G + b.n_seqs - 1) / b.n_seqs;      // of a sequence: the most, the mean
-    if (most <= kFewRows || most > kFewMostRows) return kFewRows;
-    // (a workgroup per 32 of the most rows: not where nearly all of them would be empty, nor more than a launch can have)
-    const int64_t pair_count = (int64_t)b.n_seqs * g.Hkv, blocks = pair_count * ((most + 31) / 32);
-    if (blocks > 4096 + 2 * pair_count * ((rows + 31) / 32) || blocks > (1 << 23)) return kFewRows;
-    const int tile = dtype == CASCADE_F32 ? 128 : 256;
-    const double work = (dtype == CASCADE_F32 ? 3.0 : 1.0) * g.d / 128 * (pair_count / 256.0) * longest_span(g, b);
-    return 8 + 0.36 * work * ((rows + 31) / 32) / kGroupTokens <= 28 + 3.6 * work * ((rows + tile - 1) / tile) / 64 ? kFewMostRows : kFewRows;
-}
-
 // Splits of a launch for few rows: a share is a whole number of rounds of the workgroup's waves.  A compute unit runs three workgroups (registers; four at D =
 // 64), so that many times 256 a launch, or as many times that as leave a workgroup at most 24 rounds (sequences of different lengths even out over them: 32
 // of up to 16384 keys take 61 us, with 48 rounds 90, with 12 77).
 constexpr int kFewRounds = 24;
-static FewPlan few_plan(const PagedGeom& g, const PagedBatch& b, int dtype)
+static double join_cost(int64_t rows, int64_t splits) { return 3 + rows / 1024.0 * (1 + 0.25 * splits); }      // us
+static FewPlan few_plan(const PagedGeom& g, const PagedBatch& b, int limit)
 {
     FewPlan p;
     const int64_t rows = (int64_t)b.max_new * g.G;
-    const int limit = few_rows(g, b, dtype);
     p.max_rows = rows < limit ? (int)rows : limit;
     p.block_rows = p.max_rows <= 16 ? 16 : 32;
     const int64_t pairs = (int64_t)b.n_seqs * g.Hkv, blocks = pairs * ((p.max_rows + p.block_rows - 1) / p.block_rows);
@@ -390,32 +374,60 @@ static FewPlan few_plan(const PagedGeom& g, const PagedBatch& b, int dtype)
     if (splits > most) splits = most;
     if (splits > rounds) splits = rounds;
     if (splits > kFewMaxSplits) splits = kFewMaxSplits;
-    // (the join costs 3 us and another for every 1024 rows, a round about 1: 24 new tokens of 4 heads each on 300 keys, 16 sequences, 38 us with two splits, 12 without)
-    if (splits < 1 || rounds - rounds / splits < 3 + pairs * p.max_rows / 1024) splits = 1;
+    // (a round takes about 1 us: 24 new tokens of 4 heads each on 300 keys, 16 sequences, 38 us with two splits, 12 without)
+    if (splits < 1 || rounds - rounds / splits < join_cost(pairs * p.max_rows, splits)) splits = 1;
     const int64_t each = (rounds + splits - 1) / splits;
     p.groups_per_split = (int)(each * kFewWaves);
     p.splits = (int)((rounds + each - 1) / each);
     return p;
 }
 
+// Whether the kernel for few rows takes sequences of more than kFewRows rows of a KV head too: where it is the cheaper one for the whole batch.  Its workgroups have 32 rows and
+// go over the keys again for each of them; the other kernel's have 256 (fp32: 128), one on a compute unit, begin late and take a tile of 64 keys after the other.  us, from
+// measurements of both: here 6 and 0.28 for 32 rows by 32 keys on a compute unit; there 4, 12 for a workgroup and 2 for a tile; fp32 has three times the
+// products.  bf16, d 128, 8 KV heads of 4 query heads, 16000 keys, us here and there: 16 new tokens of four sequences 52, 135; 32 of one 35, 58; 64 49, 63; 128 103, 80.
+static bool few_rows_take_all(const PagedGeom& g, const PagedBatch& b, int dtype)
+{
+    const int64_t most = (int64_t)b.max_new * g.G, rows = ((int64_t)b.n_tokens * g.G + b.n_seqs - 1) / b.n_seqs;      // of a sequence: the most, the mean
+    if (most <= kFewRows) return true;
+    // (a workgroup per 32 of the most rows: not where nearly all of them would be empty, nor more than a launch can have)
+    const int64_t pairs = (int64_t)b.n_seqs * g.Hkv, blocks = pairs * ((rows + 31) / 32), grid = pairs * ((most + 31) / 32);
+    if (grid > 4096 + 2 * blocks || grid > (1 << 23) || grid / b.n_seqs > 65535 || most > kChunkPartRows) return false;
+    const bool f32 = dtype == CASCADE_F32;
+    const int block_rows = f32 ? 128 : 256;
+    // keys of the last row, and of the mean one
+    const int64_t longest = longest_span(g, b), mean = g.window && g.window < b.max_length - b.max_new ? g.window + 32 : b.max_length - b.max_new / 2;
+    const FewPlan few = few_plan(g, b, (int)most);
+    const double here = 6 + 0.28 * (f32 ? 3 : 1) * g.d / 128 * blocks * (mean / kGroupTokens + 1) / 256 + (few.splits > 1 ? join_cost(pairs * rows, few.splits) : 0.0);
+    const ChunkPlan many = chunk_plan(g, b, 0, block_rows);
+    const double waves = ceil(pairs * ((rows + block_rows - 1) / block_rows) * many.splits / 256.0), tile = (f32 ? 3.8 : 2.0) * (g.d == 64 ? 0.75 : 1.0);
+    const double there = 4 + waves * (12 + tile * ((waves > 1 ? mean : longest) / 64.0 / many.splits + 1)) + (many.splits > 1 ? 6 : 0);
+    return here <= there;
+}
+
 size_t paged_scratch_bytes(const PagedGeom& g) { return (size_t)kChunkPartRows * (g.d + 2) * 4; }
 
 void launch_paged_attend(const PagedGeom& g, const PagedBatch& b, const void* q, int64_t q_stride, void* out, void* scratch, int dtype, hipStream_t s)
 {
-    const FewPlan p = few_plan(g, b, dtype);
     const int64_t rows = (int64_t)b.max_new * g.G;
+    const bool all = few_rows_take_all(g, b, dtype);
+    // one sequence with more: the other kernel takes it, however many of the rows there are in the end
+    const bool none = !all && b.n_seqs == 1;
+    const FewPlan p = few_plan(g, b, all ? (int)rows : kFewRows);
     with_paged_form(dtype, g.d, [&](auto f) {
         typedef typename decltype(f)::Elt T;
         constexpr int D = decltype(f)::d;
         const dim3 grid(p.splits, g.Hkv * ((p.max_rows + p.block_rows - 1) / p.block_rows), b.n_seqs);
-        if (p.block_rows == 16)
+        if (none)
+            ;
+        else if (p.block_rows == 16)
             hipLaunchKernelGGL((attend_few_kernel<T, D, 1>), grid, dim3(kFewWaves * 64), 0, s, g, b, p, (const T*)q, q_stride, (T*)out, (float*)scratch);
         else
             hipLaunchKernelGGL((attend_few_kernel<T, D, 2>), grid, dim3(kFewWaves * 64), 0, s, g, b, p, (const T*)q, q_stride, (T*)out, (float*)scratch);
-        if (p.splits > 1)
+        if (!none && p.splits > 1)
             hipLaunchKernelGGL((merge_few_kernel<T, D>), dim3(p.max_rows, g.Hkv, b.n_seqs), dim3(256), 0, s, g, b, p, (const float*)scratch, (T*)out);
-        if (rows > p.max_rows)
-            launch_attend_chunk(g, b, p.max_rows, q, q_stride, out, scratch, dtype, s);
+        if (!all)
+            launch_attend_chunk(g, b, none ? 0 : p.max_rows, q, q_stride, out, scratch, dtype, s);
     });
 }
 
