@@ -1,4 +1,4 @@
-// Attention over the paged cache in 4 bits: a few query rows per KV head (single tokens, a few of them) against a long cache.
+// Attention over the paged cache in 4 bits: blocks of a few query rows per KV head (single tokens, a few of them, short chunks) against a long cache.
 #include <type_traits>
 
 #include "async_copy.h"
@@ -33,11 +33,17 @@ constexpr int kFewStages = 2;
 template <int D> constexpr int few_stage_bytes() { return 32 * D + 256; }      // the codes, and 256 bytes from the scales on
 template <int D> constexpr int few_copies() { return D / 32 + 1; }             // copies of 1 KB, and one of 256 bytes
 
-// One group, to LDS.  The last copy's lanes behind the group (D = 64) read its last word again.
-template <int D> __device__ inline void copy_group(const uint8_t* group, uint32_t lds, int lane)
+// One group, to LDS.  The last copy's lanes behind the group (D = 64) read its last word again.  A group that one workgroup reads is streamed past the caches (32 sequences of
+// 16384 keys take 104 us, 117 without); one that other blocks of rows read too is not (33 new tokens on 60000 keys: 83 us, streamed 97).
+template <int D> __device__ inline void copy_group(const uint8_t* group, uint32_t lds, int lane, bool once)
 {
+    if (once) {
 #pragma unroll
-    for (int i = 0; i < D / 32; ++i) async_copy_1k_stream(group, (uint32_t)(i * 1024 + lane * 16), __builtin_amdgcn_readfirstlane(lds + i * 1024u));
+        for (int i = 0; i < D / 32; ++i) async_copy_1k_stream(group, (uint32_t)(i * 1024 + lane * 16), __builtin_amdgcn_readfirstlane(lds + i * 1024u));
+    } else {
+#pragma unroll
+        for (int i = 0; i < D / 32; ++i) async_copy_1k(group, (uint32_t)(i * 1024 + lane * 16), __builtin_amdgcn_readfirstlane(lds + i * 1024u));
+    }
     async_copy_256(group, (uint32_t)(32 * D + min(lane * 4, paged_group_bytes(D) - 32 * D - 4)), __builtin_amdgcn_readfirstlane(lds + 32u * D));
 }
 
@@ -94,6 +100,7 @@ template <typename T, int D, int NT> __global__ __launch_bounds__(kFewWaves * 64
     WaveRows* o_wave = (WaveRows*)ring;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), m = lane & 15, qq = lane >> 4;
     const int split = blockIdx.x, hk = blockIdx.y % g.Hkv, row0 = (gridDim.y - 1 - blockIdx.y) / g.Hkv * (16 * NT), s = blockIdx.z;
+    const bool once = NT == 1 || (int)gridDim.y == g.Hkv;      // (known to the compiler for up to 16 rows: a test of it in the loop costs 32 ragged sequences 60 -> 71 us)
     const SeqView v = seq_view(b, s);
     const int rows = v.n * g.G;
     if (row0 >= rows || rows > plan.max_rows) return;
@@ -149,7 +156,7 @@ template <typename T, int D, int NT> __global__ __launch_bounds__(kFewWaves * 64
         }
         const int at = __builtin_amdgcn_readlane(numbers, i & 63), stage = i % kFewStages;
         missing = at < 0 ? missing | 1u << stage : missing & ~(1u << stage);
-        copy_group<D>(g.pages + ((int64_t)max(at, 0) + hk * g.groups) * g.group_bytes, stages_lds + stage * kStage, lane);
+        copy_group<D>(g.pages + ((int64_t)max(at, 0) + hk * g.groups) * g.group_bytes, stages_lds + stage * kStage, lane, once);
     };
     for (int i = 0; i < min(count, kFewStages - 1); ++i) issue(i);
     for (int i = 0; i < count; ++i) {
@@ -385,7 +392,7 @@ static FewPlan few_plan(const PagedGeom& g, const PagedBatch& b, int limit)
 // Whether the kernel for few rows takes sequences of more than kFewRows rows of a KV head too: where it is the cheaper one for the whole batch.  Its workgroups have 32 rows and
 // go over the keys again for each of them; the other kernel's have 256 (fp32: 128), one on a compute unit, begin late and take a tile of 64 keys after the other.  us, from
 // measurements of both: here 6 and 0.28 for 32 rows by 32 keys on a compute unit; there 4, 12 for a workgroup and 2 for a tile; fp32 has three times the
-// products.  bf16, d 128, 8 KV heads of 4 query heads, 16000 keys, us here and there: 16 new tokens of four sequences 52, 135; 32 of one 35, 58; 64 49, 63; 128 103, 80.
+// products.  bf16, d 128, 8 KV heads of 4 query heads, 16000 keys, us here and there: 16 new tokens of four sequences 47, 135; 32 of one 31, 58; 64 43, 63; 128 about 90, 77.
 static bool few_rows_take_all(const PagedGeom& g, const PagedBatch& b, int dtype)
 {
     const int64_t most = (int64_t)b.max_new * g.G, rows = ((int64_t)b.n_tokens * g.G + b.n_seqs - 1) / b.n_seqs;      // of a sequence: the most, the mean
