@@ -297,21 +297,33 @@ template <typename T, int D, int NT> __global__ __launch_bounds__(kFewWaves * 64
 // Joins the splits of a row: the splits' maxima and sums a thread each, then D/4 threads on four channels with the splits over the rest of the workgroup.
 template <typename T, int D> __global__ __launch_bounds__(256) void merge_few_kernel(PagedGeom g, PagedBatch b, FewPlan plan, const float* __restrict__ part, T* __restrict__ out)
 {
-    constexpr int kLanes = D / 4, kParts = 256 / kLanes;
+    constexpr int kLanes = D / 4, kParts = 256 / kLanes, kFirst = 12;
     __shared__ float o_part[kParts][D], weight[kFewMaxSplits], m_wave[4], l_wave[4];
     const int row = blockIdx.x, hk = blockIdx.y, s = blockIdx.z, tid = threadIdx.x;
+    const int p = tid / kLanes, c = tid % kLanes * 4;
+    const float* x = part + ((int64_t)(s * g.Hkv + hk) * plan.splits * plan.max_rows + row) * (D + 2);
+    const int64_t step = (int64_t)plan.max_rows * (D + 2);
+    // what a launch of plan.splits may hold is on its way before the sequence is looked up: one token on 131072 keys 33.4 -> 32.3 us, on 16384 11.6 -> 11.2
+    float2 ml[2];      // of at most kFewMaxSplits, two a thread
+#pragma unroll
+    for (int i = 0; i < 2; ++i) ml[i] = tid + 256 * i < plan.splits ? *(const float2*)(x + (tid + 256 * i) * step + D) : make_float2(-INFINITY, 0.f);
+    float2 first[kFirst][2];
+#pragma unroll
+    for (int n = 0; n < kFirst; ++n) {
+        if (n * kParts >= plan.splits) break;
+        const float* y = x + min(p + n * kParts, plan.splits - 1) * step + c;
+        first[n][0] = *(const float2*)y;
+        first[n][1] = *(const float2*)(y + 2);
+    }
     const SeqView v = seq_view(b, s);
     if (row >= v.n * g.G || v.n * g.G > plan.max_rows) return;
     const int row0 = row / plan.block_rows * plan.block_rows;
     const KeySpan span = key_span(g, b, v, row0 / g.G, (min(row0 + plan.block_rows, v.n * g.G) - 1) / g.G);
     const int splits = (span.last - span.first + plan.groups_per_split - 1) / plan.groups_per_split;
     if (splits <= 1) return;      // written by its only split
-    const float* x = part + ((int64_t)(s * g.Hkv + hk) * plan.splits * plan.max_rows + row) * (D + 2);
-    const int64_t step = (int64_t)plan.max_rows * (D + 2);
-    // (at most kFewMaxSplits of them, two a thread)
-    float2 ml[2];
 #pragma unroll
-    for (int i = 0; i < 2; ++i) ml[i] = tid + 256 * i < splits ? *(const float2*)(x + (tid + 256 * i) * step + D) : make_float2(-INFINITY, 0.f);
+    for (int i = 0; i < 2; ++i)
+        if (tid + 256 * i >= splits) ml[i] = make_float2(-INFINITY, 0.f);
     float top = fmaxf(ml[0].x, ml[1].x);
 #pragma unroll
     for (int w = 32; w; w >>= 1) top = fmaxf(top, __shfl_xor(top, w));
@@ -329,17 +341,18 @@ template <typename T, int D> __global__ __launch_bounds__(256) void merge_few_ke
     for (int w = 32; w; w >>= 1) l += __shfl_xor(l, w);
     if ((tid & 63) == 0) l_wave[tid >> 6] = l;
     __syncthreads();
-    const int p = tid / kLanes, c = tid % kLanes * 4;
     float o[4] = {};
-#pragma unroll 8
-    for (int i = p; i < splits; i += kParts) {
-        const float f = weight[i];
-        const float2 a = *(const float2*)(x + i * step + c), e = *(const float2*)(x + i * step + c + 2);
+    const auto add = [&](float f, const float2& a, const float2& e) {
         o[0] += f * a.x;
         o[1] += f * a.y;
         o[2] += f * e.x;
         o[3] += f * e.y;
-    }
+    };
+#pragma unroll
+    for (int n = 0; n < kFirst; ++n)
+        if (p + n * kParts < splits) add(weight[p + n * kParts], first[n][0], first[n][1]);
+#pragma unroll 8
+    for (int i = p + kFirst * kParts; i < splits; i += kParts) add(weight[i], *(const float2*)(x + i * step + c), *(const float2*)(x + i * step + c + 2));
     *(float4*)&o_part[p][c] = make_float4(o[0], o[1], o[2], o[3]);
     __syncthreads();
     if (p) return;
