@@ -32,7 +32,10 @@ def _rows(x: torch.Tensor, device, dtype, tokens: int, heads: int, head_dim: int
         fits = x.dtype is dtype and x.device == device and x.shape == (tokens, heads, head_dim)
         assert fits and ((strides[2] == 1 or head_dim == 1) and (strides[1] == head_dim or heads == 1) or x.numel() == 0), \
             (x.device, x.dtype, tuple(x.shape), strides, "wanted", device, dtype, (tokens, heads, head_dim))
-    return strides[0] if tokens > 1 else 0
+    if tokens < 2:
+        return 0
+    assert strides[0] >= heads * head_dim, ("tokens of an array must not share memory", tuple(x.shape), strides)      # (an expanded one; 0 would stand for contiguous)
+    return strides[0]
 
 
 class RopeTable:

@@ -198,3 +198,16 @@ def test_model_rounds_to_the_nearest_code():
     codes, byte = M.quantise_k(y.reshape(-1, 1, 8).repeat(4, 1).reshape(-1, 32))
     assert byte.shape == (625, 1)
     assert (np.abs(M.k_values(codes, byte) - y.reshape(-1, 1, 8).repeat(4, 1).reshape(-1, 32)) <= 2.0 ** (byte.astype(float) - 127) * 1.0).all()
+
+
+def test_arrays_whose_tokens_share_memory_are_refused():
+    """An expanded array has stride 0, which the calls take for contiguous: it must not get that far."""
+    import torch
+    from paper_2406_17808_amd import paged
+    one = torch.zeros((1, 2, 64))
+    assert paged._rows(one, one.device, one.dtype, 1, 2, 64) == 0
+    assert paged._rows(torch.zeros((3, 5, 64))[:, 1:3], one.device, one.dtype, 3, 2, 64) == 5 * 64
+    with pytest.raises(AssertionError):
+        paged._rows(one.expand(5, -1, -1), one.device, one.dtype, 5, 2, 64)
+    with pytest.raises(AssertionError):
+        paged._rows(torch.zeros(2 * 64 + 64 * 4).as_strided((5, 2, 64), (64, 64, 1)), one.device, one.dtype, 5, 2, 64)
