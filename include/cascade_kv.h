@@ -392,13 +392,13 @@ int cascade_norm_rope(const cascade_norm_rope_args* args, void* stream);
  *   V scales at 33*head_dim: bf16 number ((r/4)%4)*8 + (r/16)*4 + r%4
  */
 typedef struct cascade_paged_config {
-    int32_t n_q_heads;         /* a multiple of n_kv_heads */
+    int32_t n_q_heads;         /* a multiple of n_kv_heads, at most 1024 */
     int32_t n_kv_heads;
     int32_t head_dim;          /* 64 or 128 */
     int32_t dtype;             /* CASCADE_F32 or CASCADE_BF16: q, k, v and outputs */
     int32_t page_size;         /* a multiple of 32, at most 65536 */
     int32_t max_seqs;          /* largest n_seqs of a batch, at most 65535 */
-    int64_t n_pages;           /* pages in dev_pages */
+    int64_t n_pages;           /* pages in dev_pages, 2^39 bytes at most */
     float softmax_scale;       /* 0 selects 1/sqrt(head_dim) */
     int32_t window;            /* 0: a query sees every token up to its own; w > 0: the last w of them */
 } cascade_paged_config;
@@ -411,6 +411,9 @@ typedef struct cascade_paged_config {
  * What goes beyond them is left out: tokens from row n_tokens on are neither written nor attended from, positions at or above max_length,
  * behind the end of the table or on a page outside [0, n_pages) are neither written nor seen.
  * Two new tokens on the same slot of the same page (a page listed twice): one of them is stored, or parts of both.
+ * Limits (BAD_ARG): n_tokens <= 2^20, max_length <= 2^31 - 2^20, and of the workgroups that a call would need,
+ * (n_tokens / 32 + 2 n_seqs) * n_kv_heads + n_tokens <= 2^22 and n_tokens * n_q_heads / 128 + n_seqs * n_kv_heads <= 2^22.
+ * Bounds far above what the arrays hold cost time: splits and kernels are chosen by them (and with them how sums are rounded).
  */
 typedef struct cascade_paged_batch {
     int32_t n_seqs;
@@ -446,7 +449,7 @@ void cascade_paged_destroy(cascade_paged_ctx* ctx);
  * whole 16-byte pieces.  n_tokens = 0 or n_seqs = 0 does nothing.  The calls advance no length: the caller does once all of a step are issued.
  * Errors: NULL_ARG, BAD_ARG, HIP.
  *
- * append: keys (rotated to their positions if the context has a table) and values of the new tokens into the pages.  dev_q (may be NULL):
+ * append: keys (rotated to their positions if the context has a table, which max_length must not pass) and values of the new tokens into the pages.  dev_q (may be NULL):
  *   their queries, rotated in the same launch into dev_q_out [n_tokens, n_q_heads, head_dim], rounded to the element type (dev_q_out may be
  *   dev_q if that is contiguous); needs the table.
  * attend: dev_out[t] = softmax attention of query t (already rotated) over its sequence's positions up to its own (within the window).

@@ -106,7 +106,8 @@ __device__ inline double2 rope_or_nan(const PagedGeom& g, int half, int p, int i
 
 // A workgroup per new token.  Rows are the KV heads' keys, their values and the query heads, D / 16 threads a row: the cosines and
 // sines are made once per token, in 64 bits, and every row is read in 16-byte pieces.  Keys are rotated and
-// rounded to codes in 64 bits: their codes then depend on nothing but the row and its position.
+// rounded to codes in 64 bits: their codes then depend on nothing but the row and its position.  32 single tokens of 32 + 8 + 8 heads (0.8 MB): 4.8 us on
+// the device, the latency of arrays, table and row one after the other.
 template <typename T, int D> __global__ __launch_bounds__(1024) void append_token_kernel(PagedGeom g, PagedBatch b, PagedRows x)
 {
     constexpr int kTpr = D / 16, half = D / 2;
@@ -172,7 +173,8 @@ __device__ inline GroupRows group_rows(const SeqView& v, int number)
 
 // Many tokens of a sequence: a workgroup per group of 32 tokens and KV head, D / 16 threads a row, one half of the workgroup on keys and the other on
 // values.  V bytes are gathered in LDS and leave in 16-byte pieces (a group that is not filled: in words of four tokens, or bytes); written
-// token by token they are bytes 16 apart.  Workgroups behind the groups rotate queries, a row of D / 16 threads each.
+// token by token they are bytes 16 apart.  Workgroups behind the groups rotate queries, a row of D / 16 threads each.  4096 tokens of 8 KV heads, d 128, bf16: 23.0 us with the
+// queries of 32 heads (88 MB, 3.8 TB/s), 15 without: the rounding of keys in 64 bits; a workgroup per token takes 27.
 template <typename T, int D> __global__ __launch_bounds__(4 * D) void append_group_kernel(PagedGeom g, PagedBatch b, PagedRows x, unsigned group_blocks)
 {
     constexpr int kTpr = D / 16, half = D / 2, kHalf = 2 * D;      // threads of a half of the workgroup: 32 rows
@@ -236,7 +238,7 @@ template <typename T, int D> __global__ __launch_bounds__(4 * D) void append_gro
     }
 }
 
-// Reading many tokens of a sequence: the same workgroups the other way round.
+// Reading many tokens of a sequence: the same workgroups the other way round (4096 tokens, 21 MB: 9.2 us; a workgroup per token 11.6).
 template <typename T, int D> __global__ __launch_bounds__(4 * D) void read_group_kernel(PagedGeom g, PagedBatch b, void* k_out, void* v_out)
 {
     constexpr int kTpr = D / 16, kHalf = 2 * D;
@@ -312,7 +314,8 @@ static int row_threads(int rows, int d)
     return n > 1024 ? 1024 : n;
 }
 
-// Sequences with at least this many new tokens are written group by group: a launch is one kernel for all its sequences, by max_new.
+// Calls with a sequence of at least this many new tokens go group by group: a launch is one kernel for all its sequences, by max_new (a group with a few
+// tokens leaves most of its workgroup idle).
 constexpr int kGroupFormTokens = 16;
 
 // At least the groups that all sequences reach.
