@@ -19,7 +19,7 @@ namespace ckv {
 // A workgroup has kFewWaves waves; wave w takes groups w, w + kFewWaves, ... of the workgroup's share.  A wave has kFewStages groups of its own in
 // LDS, filled by asynchronous copies (a group is contiguous), and waits only for its own.  A group takes a wave 1 to 2 us from its first LDS read to its last product, most of it
 // waiting for itself, so waves a SIMD count for more than bytes on their way: 32 sequences of 16384 keys (562 MB) take 104 us with two
-// stages and three workgroups a compute unit, 106 with three stages, 114 with four and two workgroups; 132 with the next group's
+// stages, 106 with three stages, 114 with four and two workgroups; 132 with the next group's
 // loads in registers.  One token on 131072 keys (140 MB): 25 us and 5 for the join of 94 splits, 5.6 and 4.4 TB/s; a large copy reaches 4.74.  The running maximum is raised only when a logit exceeds it by 2^8 (in 32 bits nothing is lost below 2^127): a
 // vote instead of an exchange between lanes for most groups.
 template <int D> struct GroupCodes {
@@ -375,12 +375,14 @@ static int64_t longest_span(const PagedGeom& g, const PagedBatch& b)
     return g.window && g.window < b.max_length - b.max_new ? (int64_t)g.window + b.max_new : b.max_length;
 }
 
-// Splits of a launch for few rows: a share is a whole number of rounds of the workgroup's waves.  A compute unit runs three workgroups (registers; four at D =
-// 64), so that many times 256 a launch, or as many times that as leave a workgroup at most 24 rounds (sequences of different lengths even out over them: 32
-// of up to 16384 keys take 61 us, with 48 rounds 90, with 12 77).
+// Splits of a launch for few rows: a share is a whole number of rounds of the workgroup's waves.  Workgroups that a compute unit runs at once: with 16 rows, bound by
+// memory, three are enough (registers would allow four: one token on 131072 keys 32.3 us, with four 34.7; at D = 64 four); with 32 rows two (three at D
+// = 64), fp32 one (two).  That many times 256 a launch (16 new tokens of four sequences on 16000 keys: 41 us, with three workgroups a unit 47; fp32 on 2000 keys
+// 18, with two 24), or as many times that as leave a workgroup at most 24 rounds (sequences of different lengths even out over them: 32 of up to 16384 keys take 60
+// us, with 48 rounds 90, with 12 77).
 constexpr int kFewRounds = 24;
 static double join_cost(int64_t rows, int64_t splits) { return 3 + rows / 1024.0 * (1 + 0.25 * splits); }      // us
-static FewPlan few_plan(const PagedGeom& g, const PagedBatch& b, int limit)
+static FewPlan few_plan(const PagedGeom& g, const PagedBatch& b, int limit, int dtype)
 {
     FewPlan p;
     const int64_t rows = (int64_t)b.max_new * g.G;
@@ -388,7 +390,8 @@ static FewPlan few_plan(const PagedGeom& g, const PagedBatch& b, int limit)
     p.block_rows = p.max_rows <= 16 ? 16 : 32;
     const int64_t pairs = (int64_t)b.n_seqs * g.Hkv, blocks = pairs * ((p.max_rows + p.block_rows - 1) / p.block_rows);
     const int64_t rounds = (longest_span(g, b) / kGroupTokens + 2 + kFewWaves - 1) / kFewWaves;      // of the longest sequence (its first and last group may be begun)
-    const int64_t fill = g.d == 64 ? 1024 : 768, most = kChunkPartRows / (pairs * p.max_rows);      // (the partial results have to fit)
+    const int at_once = p.block_rows == 16 ? 3 : dtype == CASCADE_F32 ? 1 : 2;
+    const int64_t fill = 256 * (g.d == 64 ? at_once + 1 : at_once), most = kChunkPartRows / (pairs * p.max_rows);      // (the partial results have to fit)
     int64_t splits = fill / blocks;
     for (int64_t k = 2; splits < most && rounds > kFewRounds * (splits < 1 ? 1 : splits) && k <= 64; ++k) splits = fill * k / blocks;
     if (splits > most) splits = most;
@@ -405,7 +408,7 @@ static FewPlan few_plan(const PagedGeom& g, const PagedBatch& b, int limit)
 // Whether the kernel for few rows takes sequences of more than kFewRows rows of a KV head too: where it is the cheaper one for the whole batch.  Its workgroups have 32 rows and
 // go over the keys again for each of them; the other kernel's have 256 (fp32: 128), one on a compute unit, begin late and take a tile of 64 keys after the other.  us, from
 // measurements of both: here 6 and 0.28 for 32 rows by 32 keys on a compute unit; there 4, 12 for a workgroup and 2 for a tile; fp32 has three times the
-// products.  bf16, d 128, 8 KV heads of 4 query heads, 16000 keys, us here and there: 16 new tokens of four sequences 47, 135; 32 of one 31, 58; 64 43, 63; 128 about 90, 77.
+// products.  bf16, d 128, 8 KV heads of 4 query heads, 16000 keys, us here and there: 16 new tokens of four sequences 41, 135; 32 of one 27, 58; 64 39, 63; 128 about 90, 77.
 static bool few_rows_take_all(const PagedGeom& g, const PagedBatch& b, int dtype)
 {
     const int64_t most = (int64_t)b.max_new * g.G, rows = ((int64_t)b.n_tokens * g.G + b.n_seqs - 1) / b.n_seqs;      // of a sequence: the most, the mean
@@ -417,7 +420,7 @@ static bool few_rows_take_all(const PagedGeom& g, const PagedBatch& b, int dtype
     const int block_rows = f32 ? 128 : 256;
     // keys of the last row, and of the mean one
     const int64_t longest = longest_span(g, b), mean = g.window && g.window < b.max_length - b.max_new ? g.window + 32 : b.max_length - b.max_new / 2;
-    const FewPlan few = few_plan(g, b, (int)most);
+    const FewPlan few = few_plan(g, b, (int)most, dtype);
     const double here = 6 + 0.28 * (f32 ? 3 : 1) * g.d / 128 * blocks * (mean / kGroupTokens + 1) / 256 + (few.splits > 1 ? join_cost(pairs * rows, few.splits) : 0.0);
     const ChunkPlan many = chunk_plan(g, b, 0, block_rows);
     const double waves = ceil(pairs * ((rows + block_rows - 1) / block_rows) * many.splits / 256.0), tile = (f32 ? 3.8 : 2.0) * (g.d == 64 ? 0.75 : 1.0);
@@ -433,7 +436,7 @@ void launch_paged_attend(const PagedGeom& g, const PagedBatch& b, const void* q,
     const bool all = few_rows_take_all(g, b, dtype);
     // one sequence with more: the other kernel takes it, however many of the rows there are in the end
     const bool none = !all && b.n_seqs == 1;
-    const FewPlan p = few_plan(g, b, all ? (int)rows : kFewRows);
+    const FewPlan p = few_plan(g, b, all ? (int)rows : kFewRows, dtype);
     with_paged_form(dtype, g.d, [&](auto f) {
         typedef typename decltype(f)::Elt T;
         constexpr int D = decltype(f)::d;
