@@ -368,6 +368,38 @@ template <typename T, int D> __global__ __launch_bounds__(256) void merge_few_ke
     store4(out + ((int64_t)(v.first + i) * g.Hq + hk * g.G + h) * D + c, o[0] * r, o[1] * r, o[2] * r, o[3] * r);
 }
 
+// The same for a few splits of many rows: D/4 threads a row, one split after the other.
+template <typename T, int D> __global__ __launch_bounds__(256) void merge_rows_kernel(PagedGeom g, PagedBatch b, FewPlan plan, const float* __restrict__ part, T* __restrict__ out)
+{
+    constexpr int kLanes = D / 4;
+    const int row = blockIdx.x * (256 / kLanes) + threadIdx.x / kLanes, hk = blockIdx.y, s = blockIdx.z, c = threadIdx.x % kLanes * 4;
+    const SeqView v = seq_view(b, s);
+    if (row >= v.n * g.G || v.n * g.G > plan.max_rows) return;
+    const int row0 = row / plan.block_rows * plan.block_rows;
+    const KeySpan span = key_span(g, b, v, row0 / g.G, (min(row0 + plan.block_rows, v.n * g.G) - 1) / g.G);
+    const int splits = (span.last - span.first + plan.groups_per_split - 1) / plan.groups_per_split;
+    if (splits <= 1) return;
+    const float* x = part + ((int64_t)(s * g.Hkv + hk) * plan.splits * plan.max_rows + row) * (D + 2);
+    const int64_t step = (int64_t)plan.max_rows * (D + 2);
+    float top = -INFINITY;
+#pragma unroll 4
+    for (int i = 0; i < splits; ++i) top = fmaxf(top, x[i * step + D]);
+    float l = 0.f, o[4] = {};
+#pragma unroll 4
+    for (int i = 0; i < splits; ++i) {
+        const float2 a = *(const float2*)(x + i * step + c), e = *(const float2*)(x + i * step + c + 2), ml = *(const float2*)(x + i * step + D);
+        const float f = ml.x == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(ml.x - top);
+        l += f * ml.y;
+        o[0] += f * a.x;
+        o[1] += f * a.y;
+        o[2] += f * e.x;
+        o[3] += f * e.y;
+    }
+    const int i = row / g.G, h = row - i * g.G;
+    const float r = top == -INFINITY ? 0.f : 1.f / l;
+    store4(out + ((int64_t)(v.first + i) * g.Hq + hk * g.G + h) * D + c, o[0] * r, o[1] * r, o[2] * r, o[3] * r);
+}
+
 // ------------------------------------------------------------------ launches
 // The longest range of keys of a batch's sequences.
 static int64_t longest_span(const PagedGeom& g, const PagedBatch& b)
@@ -381,7 +413,10 @@ static int64_t longest_span(const PagedGeom& g, const PagedBatch& b)
 // 18, with two 24), or as many times that as leave a workgroup at most 24 rounds (sequences of different lengths even out over them: 32 of up to 16384 keys take 60
 // us, with 48 rounds 90, with 12 77).
 constexpr int kFewRounds = 24;
-static double join_cost(int64_t rows, int64_t splits) { return 3 + rows / 1024.0 * (1 + 0.25 * splits); }      // us
+// Joins of at least 2048 rows of at most 16 splits go to merge_rows_kernel (16 new tokens of four sequences on 16000 keys, 2048 rows of 16 splits: 39 us in all, with
+// a workgroup a row 42; 1024 rows of 9 splits 61 and 60; 512 of 16 21 and 20; 32 7.8 and 7.5).
+static bool rows_share_workgroups(int64_t rows, int64_t splits) { return rows >= 2048 && splits <= 16; }
+static double join_cost(int64_t rows, int64_t splits) { return 5 + rows / 1024.0 * (rows_share_workgroups(rows, splits) ? 0.2 * splits : 1 + 0.25 * splits); }      // us
 static FewPlan few_plan(const PagedGeom& g, const PagedBatch& b, int limit, int dtype)
 {
     FewPlan p;
@@ -447,7 +482,9 @@ void launch_paged_attend(const PagedGeom& g, const PagedBatch& b, const void* q,
             hipLaunchKernelGGL((attend_few_kernel<T, D, 1>), grid, dim3(kFewWaves * 64), 0, s, g, b, p, (const T*)q, q_stride, (T*)out, (float*)scratch);
         else
             hipLaunchKernelGGL((attend_few_kernel<T, D, 2>), grid, dim3(kFewWaves * 64), 0, s, g, b, p, (const T*)q, q_stride, (T*)out, (float*)scratch);
-        if (!none && p.splits > 1)
+        if (!none && p.splits > 1 && rows_share_workgroups((int64_t)b.n_seqs * g.Hkv * p.max_rows, p.splits))
+            hipLaunchKernelGGL((merge_rows_kernel<T, D>), dim3((p.max_rows * D / 4 + 255) / 256, g.Hkv, b.n_seqs), dim3(256), 0, s, g, b, p, (const float*)scratch, (T*)out);
+        else if (!none && p.splits > 1)
             hipLaunchKernelGGL((merge_few_kernel<T, D>), dim3(p.max_rows, g.Hkv, b.n_seqs), dim3(256), 0, s, g, b, p, (const float*)scratch, (T*)out);
         if (!all)
             launch_attend_chunk(g, b, none ? 0 : p.max_rows, q, q_stride, out, scratch, dtype, s);
