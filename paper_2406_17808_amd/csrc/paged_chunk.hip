@@ -142,7 +142,7 @@ template <typename T, int D, int NW> __global__ __launch_bounds__(NW * 64, 1) vo
         }
         const bool is_k = wave + NW * i < 4;
         uint32_t at = __builtin_amdgcn_readlane(places[i], t & 63);
-        held[i].gone = !decltype(plain)::value && at == ~0u;
+        held[i].gone = !decltype(plain)::value && missing && at == ~0u;      // (what no row sees is masked anyway, and the fast form leaves gone_lds as it is)
         at = min(at, last_place);      // a group that is missing: any other's bytes, which nobody sees
         const uint8_t* group = g.pages + ((uint64_t)at << 7);
         held[i].load(group + (is_k ? 0 : 16 * D) + n * (4 * kWords));
