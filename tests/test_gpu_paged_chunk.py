@@ -7,7 +7,8 @@ import math
 import pytest
 import torch
 
-from test_gpu_paged import Run, attend_case
+from paper_2406_17808_amd import paged
+from test_gpu_paged import attend_case
 
 pytestmark = pytest.mark.gpu
 
@@ -117,3 +118,59 @@ def test_a_long_chunk_of_many_heads(dtype):
     new = 512 if dtype == "bf16" else 250
     run, batch, q, out = attend_case(dtype, 128, 32, 8, 128, [6000 - new], [new], seed=4)
     run.check_attend(batch, q, out)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("new", [3, 70])
+def test_one_sequence_under_a_large_bound(dtype, new):
+    """The host names far more new tokens of a single sequence than there are: the kernel for many rows takes them, rows of no sequence stay."""
+    run, batch, q, _ = attend_case(dtype, 128, 32, 8, 64, [700], [new], seed=new)
+    more = torch.cat([q, q[:1].expand(2000, -1, -1)])
+    wide = paged.PagedBatch(batch.lengths, batch.new_offsets, batch.page_table, new + 2000, 2000, 9000)
+    got = torch.full_like(more, 3.0)
+    run.cache.attend(wide, more, out=got)
+    run.check_attend(batch, q, got[:new])
+    assert bool((got[new:] == 3).all())
+
+
+@pytest.mark.parametrize("lengths,new,empty", [([3000], [90], 99), ([700, 0, 1], [400, 0, 257], 420), ([1500, 0, 900, 40], [32, 32, 1, 5], 4)])
+def test_captured_and_replayed(lengths, new, empty):
+    """All forms of a call from a graph, replayed between eager calls of the same cache on other inputs and with other lengths."""
+    lengths, new = with_empty(lengths, new, empty)
+    run, batch, q, out = attend_case("bf16", 128, 16, 2, 64, lengths, new, seed=1)
+    k, v = run.rows(sum(new), 2), run.rows(sum(new), 2)
+    q2, pages = run.rows(sum(new), 16), run.cache.pages.clone()
+    run.cache.append(batch, k, v)
+    after, want_k, want_v = run.cache.attend(batch, q), *run.cache.read(batch)
+    shorter = batch.lengths.clone()
+    shorter[0] -= 40
+    got, stream = torch.empty_like(q), torch.cuda.Stream()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=stream):
+        before = run.cache.attend(batch, q)
+        run.cache.append(batch, k, v)
+        run.cache.attend(batch, q, out=got)
+        got_k, got_v = run.cache.read(batch)
+    for i in range(4):
+        run.cache.pages.copy_(pages)
+        for x in (before, got, got_k, got_v):
+            x.zero_()
+        other = run.cache.attend(batch, q2)
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(before, out) and torch.equal(got, after), i
+        assert torch.equal(got_k, want_k) and torch.equal(got_v, want_v) and other.isfinite().all()
+    # what the graph reads when it runs
+    was = batch.lengths.clone()
+    run.cache.pages.copy_(pages)
+    batch.lengths.copy_(shorter)
+    graph.replay()
+    torch.cuda.synchronize()
+    assert torch.equal(before, run_at(run, batch, q, pages)), "follows the lengths"
+    batch.lengths.copy_(was)
+
+
+def run_at(run, batch, q, pages):
+    run.cache.pages.copy_(pages)
+    return run.cache.attend(batch, q)
