@@ -81,6 +81,47 @@ template <typename T, int D, int NW> __global__ __launch_bounds__(NW * 64, 1) vo
     }
     const int NT = tile1 - tile0;
 
+    // ---- codes -> LDS
+    // item i of a wave is pieces 64 (w % 2) .. of group w / 2 % 2, w = wave + NW * i; K for w < 4 (of a thread: the same piece of K and V)
+    const int n = (wave & 1) * 64 + l, gi = (wave & 3) >> 1;
+    // K, D = 128: block n / 32 of key n % 32; D = 64: half n % 2 of block n / 64 of key n / 2 % 32.  Its scale's byte stands next to that of the key 16 apart.
+    const int key = D == 128 ? n & 31 : (n >> 1) & 31, k_block = D == 128 ? n >> 5 : n >> 6;
+    const int k_to = k_place<D>(32 * gi + key, D == 128 ? 4 * k_block : 4 * k_block + 2 * (n & 1)) * 2;      // bytes; its pieces of 8 channels: XOR 16 e
+    // V, D = 128: chunk n / 64, keys 4q + b, 16 + 4q + b with q = n / 16 % 4, channels n % 16 + 16 (0 .. 3) of 64; D = 64: half of that
+    const int c16 = D == 128 ? n : n >> 1, v_to = v_place((D == 128 ? 64 * (n >> 6) : 32 * (n & 1)) + (c16 & 15), 4 * gi + ((c16 >> 4) & 3)) * 2;
+    auto tile_of = [&](int item, int set) { return wave + NW * item < 4 ? set + 1 : set; };
+    Piece<kWords> held[kItems];
+    // lane l: place of the item's group in tile 64 * k + l, in units of 128 bytes; ~0: the group is missing
+    uint32_t places[kItems];
+    bool missing = false;      // a group that some row sees is
+    constexpr uint32_t kGroupUnits = paged_group_bytes(D) / 128;
+    const uint32_t last_place = (uint32_t)(g.n_pages * g.Hkv * g.groups - 1) * kGroupUnits;
+    auto find_places = [&](int i, int t) {
+        const int64_t at = t + l < NT ? paged_group(g, b, s, ((tile0 + t + l) * 2 + gi) * kGroupTokens) : -1;
+        places[i] = at < 0 ? ~0u : (uint32_t)(at + (int64_t)hk * g.groups) * kGroupUnits;
+    };
+    auto load_tile = [&](int i, int t, auto plain) {
+        if (__builtin_expect((t & 63) == 0 && t > 0, 0)) find_places(i, t);
+        const bool is_k = wave + NW * i < 4;
+        uint32_t at = __builtin_amdgcn_readlane(places[i], t & 63);
+        held[i].gone = !decltype(plain)::value && at == ~0u;
+        at = min(at, last_place);      // a group that is missing: any other's bytes, which nobody sees
+        const uint8_t* group = g.pages + ((uint64_t)at << 7);
+        held[i].load(group + (is_k ? 0 : 16 * D) + n * (4 * kWords));
+        held[i].extra = *(const uint16_t*)(group + (is_k ? 32 * D + k_block * 32 + (key & 15) * 2 : 33 * D + 2 * l32));
+    };
+    auto load_set = [&](int set) {
+#pragma unroll
+        for (int i = 0; i < kItems; ++i) {
+            const int t = tile_of(i, set);
+            if (t >= 0 && t < NT) load_tile(i, t, std::false_type());
+        }
+    };
+    // The first loads are on their way together with the queries: the places of 64 tiles, then this wave's piece of tile 0.
+    const int lead = late ? 2 : 1;      // a wave converts set t + lead in vector block t + 1
+    find_places(0, 0);
+    places[kItems - 1] = places[0];
+    load_set(lead - 2);
     Frag qf[kTerms][KS];
     {
         const int r = min(row, rows - 1), i = r / g.G, h = r - i * g.G;
@@ -113,41 +154,17 @@ template <typename T, int D, int NW> __global__ __launch_bounds__(NW * 64, 1) vo
 
     // Whether anything in the range needs the careful form of a tile: a group that is missing (looked for here), a V row of NaN (seen when it is
     // converted).  It stays set: the fast form ends for the rest.
-    bool missing = false;
-    for (int i = tid; i < 2 * NT; i += NW * 64) {
+    auto absent = [&](int i, bool there) {      // group i of the range, seen by some row
         const int p = (2 * tile0 + i) * kGroupTokens;
-        missing |= p < to_of(pos_of(row0 + kRows - 1)) && p + kGroupTokens > from_of(pos_of(row0)) && paged_group(g, b, s, p) < 0;
-    }
+        return i < 2 * NT && p < to_of(pos_of(row0 + kRows - 1)) && p + kGroupTokens > from_of(pos_of(row0)) && !there;
+    };
+    missing = absent(2 * l + gi, places[0] != ~0u);      // (the waves have both groups of 64 tiles)
+    for (int i = 128 + tid; i < 2 * NT; i += NW * 64) missing |= absent(i, paged_group(g, b, s, (2 * tile0 + i) * kGroupTokens) >= 0);
     missing = __syncthreads_or(missing);
     if (tid == 0) special_lds = missing;
 
-    // ---- codes -> LDS
-    // item i of a wave is pieces 64 (w % 2) .. of group w / 2 % 2, w = wave + NW * i; K for w < 4 (of a thread: the same piece of K and V)
-    const int n = (wave & 1) * 64 + l, gi = (wave & 3) >> 1;
-    // K, D = 128: block n / 32 of key n % 32; D = 64: half n % 2 of block n / 64 of key n / 2 % 32.  Its scale's byte stands next to that of the key 16 apart.
-    const int key = D == 128 ? n & 31 : (n >> 1) & 31, k_block = D == 128 ? n >> 5 : n >> 6;
-    const int k_to = k_place<D>(32 * gi + key, D == 128 ? 4 * k_block : 4 * k_block + 2 * (n & 1)) * 2;      // bytes; its pieces of 8 channels: XOR 16 e
-    // V, D = 128: chunk n / 64, keys 4q + b, 16 + 4q + b with q = n / 16 % 4, channels n % 16 + 16 (0 .. 3) of 64; D = 64: half of that
-    const int c16 = D == 128 ? n : n >> 1, v_to = v_place((D == 128 ? 64 * (n >> 6) : 32 * (n & 1)) + (c16 & 15), 4 * gi + ((c16 >> 4) & 3)) * 2;
-    auto tile_of = [&](int item, int set) { return wave + NW * item < 4 ? set + 1 : set; };
-    Piece<kWords> held[kItems];
-    // lane l: place of the item's group in tile 64 * k + l, in units of 128 bytes; ~0: the group is missing
-    uint32_t places[kItems];
-    constexpr uint32_t kGroupUnits = paged_group_bytes(D) / 128;
-    const uint32_t last_place = (uint32_t)(g.n_pages * g.Hkv * g.groups - 1) * kGroupUnits;
-    auto load_tile = [&](int i, int t, auto plain) {
-        if (__builtin_expect((t & 63) == 0, 0)) {
-            const int64_t at = t + l < NT ? paged_group(g, b, s, ((tile0 + t + l) * 2 + gi) * kGroupTokens) : -1;
-            places[i] = at < 0 ? ~0u : (uint32_t)(at + (int64_t)hk * g.groups) * kGroupUnits;
-        }
-        const bool is_k = wave + NW * i < 4;
-        uint32_t at = __builtin_amdgcn_readlane(places[i], t & 63);
-        held[i].gone = !decltype(plain)::value && missing && at == ~0u;      // (what no row sees is masked anyway, and the fast form leaves gone_lds as it is)
-        at = min(at, last_place);      // a group that is missing: any other's bytes, which nobody sees
-        const uint8_t* group = g.pages + ((uint64_t)at << 7);
-        held[i].load(group + (is_k ? 0 : 16 * D) + n * (4 * kWords));
-        held[i].extra = *(const uint16_t*)(group + (is_k ? 32 * D + k_block * 32 + (key & 15) * 2 : 33 * D + 2 * l32));
-    };
+    // (what no row sees is masked anyway, and the fast form leaves gone_lds as it is)
+    auto is_gone = [&](int i, auto plain) { return !decltype(plain)::value && missing && held[i].gone; };
     auto write_codes = [&](int i, int stage, auto plain) {
         const Piece<kWords>& x = held[i];
         if (wave + NW * i < 4) {
@@ -166,18 +183,11 @@ template <typename T, int D, int NW> __global__ __launch_bounds__(NW * 64, 1) vo
         }
         if (wave & 1) return;
         // a NaN must not reach rows that do not see the key (0 * NaN): the scale becomes 0, and rows that do see it are marked
-        const bool finite = (x.extra & 0x7F80u) != 0x7F80u;
-        vs_lds[stage][32 * gi + l32] = finite && !x.gone ? __uint_as_float(x.extra << 16) : 0.f;
-        const uint32_t odd = x.gone ? 0u : (uint32_t)__ballot(!finite);      // lanes 32 .. 63 have the same scales
+        const bool finite = (x.extra & 0x7F80u) != 0x7F80u, gone = is_gone(i, plain);
+        vs_lds[stage][32 * gi + l32] = finite && !gone ? __uint_as_float(x.extra << 16) : 0.f;
+        const uint32_t odd = gone ? 0u : (uint32_t)__ballot(!finite);      // lanes 32 .. 63 have the same scales
         if (__builtin_expect(odd != 0u, 0)) special_lds = 1;
         if (!decltype(plain)::value || __builtin_expect(odd != 0u, 0)) odd_lds[stage][gi] = odd;      // (0 as long as nothing was special)
-    };
-    auto load_set = [&](int set) {
-#pragma unroll
-        for (int i = 0; i < kItems; ++i) {
-            const int t = tile_of(i, set);
-            if (t >= 0 && t < NT) load_tile(i, t, std::false_type());
-        }
     };
     auto write_set = [&](int set) {
 #pragma unroll
@@ -185,7 +195,7 @@ template <typename T, int D, int NW> __global__ __launch_bounds__(NW * 64, 1) vo
             const int t = tile_of(i, set);
             if (t < 0 || t >= NT) continue;
             write_codes(i, set & 1, std::false_type());
-            if (wave + NW * i < 4 && !(wave & 1) && l == 0) gone_lds[set & 1][gi] = held[i].gone;
+            if (wave + NW * i < 4 && !(wave & 1) && l == 0) gone_lds[set & 1][gi] = is_gone(i, std::false_type());
         }
     };
 
@@ -308,17 +318,13 @@ template <typename T, int D, int NW> __global__ __launch_bounds__(NW * 64, 1) vo
             for (int j = 0; j < 16; ++j) st[kb][j] = __builtin_amdgcn_exp2f(__builtin_fmaf(st[kb][j], scale, -ref));
     };
 
-    // ---- the tiles.  A wave converts set t + lead in vector block t + 1.
-    const int lead = late ? 2 : 1;
+    // ---- the tiles
     for (int i = tid; i < kBN * D / 8; i += NW * 64) *(u32x4_t*)&v_lds[1][8 * i] = u32x4_t{0, 0, 0, 0};      // matrix block -1 multiplies them with 0
     if (tid < kBN) vs_lds[1][tid] = 0.f;
     if (tid < 2) odd_lds[1][tid] = 0;
     wait_lds_reads();
     wg_barrier();      // (special_lds as well: a wave that converts may set it)
-    for (int set = -1; set < lead - 1; ++set) {
-        load_set(set);
-        write_set(set);
-    }
+    write_set(lead - 2);
     load_set(lead - 1);
     // the tiles that some row of the wave sees
     const int a0 = max(any_from / kBN - tile0, 0), a1 = min((any_to + kBN - 1) / kBN - tile0, NT);
