@@ -20,7 +20,7 @@ namespace ckv {
 // LDS, filled by asynchronous copies (a group is contiguous), and waits only for its own.  A group takes a wave 1 to 2 us from its first LDS read to its last product, most of it
 // waiting for itself, so waves a SIMD count for more than bytes on their way: 32 sequences of 16384 keys (562 MB) take 104 us with two
 // stages, 106 with three stages, 114 with four and two workgroups; 132 with the next group's
-// loads in registers.  One token on 131072 keys (140 MB): 25 us and 5 for the join of 94 splits, 5.6 and 4.4 TB/s; a large copy reaches 4.74.  The running maximum is raised only when a logit exceeds it by 2^8 (in 32 bits nothing is lost below 2^127): a
+// loads in registers.  One token on 131072 keys (140 MB): 26 us and 4 for the join of 94 splits, 5.4 and 4.6 TB/s; a large copy reaches 4.74.  The running maximum is raised only when a logit exceeds it by 2^8 (in 32 bits nothing is lost below 2^127): a
 // vote instead of an exchange between lanes for most groups.
 template <int D> struct GroupCodes {
     u32x4_t k[2];            // D = 64: the first two words

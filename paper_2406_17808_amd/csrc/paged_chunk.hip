@@ -20,8 +20,8 @@ namespace ckv {
 // 2x + 1, and set x + 2 is written from phase 2x + 2 on: two stages do.
 // What bounds it: 2048 tokens of 32 heads on 63500 cached ones, d 128, bf16, 2.0 ms: 1.08 PFLOP/s (a large library product in bf16: 1.27); the matrix cores are busy 49 % of the
 // cycles, and a wave issues an instruction every five to six cycles: its vector block (exponentials, codes, maxima) takes 2300 cycles, its matrix block
-// 1650, so that the vector blocks set the pace and each matrix block waits for one.  4096 tokens on none: 156 us, 0.89 PFLOP/s (the tiles at the diagonal,
-// and 12 us before a workgroup's first product).
+// 1650, so that the vector blocks set the pace and each matrix block waits for one.  4096 tokens on none: 153 us, 0.90 PFLOP/s (the tiles at the diagonal,
+// and about 10 us before a workgroup's first product).
 // NW = 4 (fp32: queries and scaled probabilities are sums of three bf16 terms, three times the products and the query registers): all waves are early and convert
 // K and V.
 

@@ -174,7 +174,8 @@ __device__ inline GroupRows group_rows(const SeqView& v, int number)
 // Many tokens of a sequence: a workgroup per group of 32 tokens and KV head, D / 16 threads a row, one half of the workgroup on keys and the other on
 // values.  V bytes are gathered in LDS and leave in 16-byte pieces (a group that is not filled: in words of four tokens, or bytes); written
 // token by token they are bytes 16 apart.  Workgroups behind the groups rotate queries, a row of D / 16 threads each.  4096 tokens of 8 KV heads, d 128, bf16: 23.0 us with the
-// queries of 32 heads (88 MB, 3.8 TB/s), 15 without: the rounding of keys in 64 bits; a workgroup per token takes 27.
+// queries of 32 heads (88 MB, 3.8 TB/s), 15 without: 4200 vector instructions a workgroup, most of them for the keys in 64 bits (loading the cosines ahead costs half of the
+// waves: 28 us); a workgroup per token takes 27.
 template <typename T, int D> __global__ __launch_bounds__(4 * D) void append_group_kernel(PagedGeom g, PagedBatch b, PagedRows x, unsigned group_blocks)
 {
     constexpr int kTpr = D / 16, half = D / 2, kHalf = 2 * D;      // threads of a half of the workgroup: 32 rows
