@@ -108,9 +108,11 @@ class PagedBatch:
 
 class PagedKVCache:
     """Pages of keys and values in 4 bits (see cascade_paged_config for the numbers and bytes).  `pages` [n_pages, page bytes] uint8 may be handed in;
-    with `rope` append rotates keys, and the queries given to it, to their positions."""
+    with `rope` append rotates keys, and the queries given to it, to their positions.  `workspace` (uint8, workspace_size(cfg) bytes) may be shared by layers
+    whose calls follow each other."""
 
-    def __init__(self, cfg: B.cascade_paged_config, device: str = "cuda:0", pages: Optional[torch.Tensor] = None, rope: Optional[RopeTable] = None):
+    def __init__(self, cfg: B.cascade_paged_config, device: str = "cuda:0", pages: Optional[torch.Tensor] = None, rope: Optional[RopeTable] = None,
+                 workspace: Optional[torch.Tensor] = None):
         self.cfg, self.rope = cfg, rope
         self.n_q_heads, self.n_kv_heads, self.head_dim = cfg.n_q_heads, cfg.n_kv_heads, cfg.head_dim
         self.device = torch.device(device)
@@ -124,10 +126,18 @@ class PagedKVCache:
         assert pages.device == self.device and pages.dtype == torch.uint8 and tuple(pages.shape) == (cfg.n_pages, self.page_bytes) and pages.is_contiguous()
         assert rope is None or (rope.device == self.device and rope.head_dim == cfg.head_dim)
         self.pages = pages
-        self.workspace = torch.empty(self.workspace_bytes + 256, dtype=torch.uint8, device=self.device)
+        if workspace is None:
+            workspace = torch.empty(self.workspace_size(cfg), dtype=torch.uint8, device=self.device)
+        assert workspace.device == self.device and workspace.dtype == torch.uint8 and workspace.is_contiguous()
+        assert workspace.numel() >= self.workspace_size(cfg), "the workspace is smaller than workspace_size(cfg)"
+        self.workspace = workspace
         with torch.cuda.device(self.device):
             self.ctx = B.cascade_paged_init(cfg, pages.data_ptr(), (self.workspace.data_ptr() + 255) & ~255, self.workspace_bytes,
                                             rope.table.data_ptr() if rope is not None else 0, rope.n_positions if rope is not None else 0)
+
+    @staticmethod
+    def workspace_size(cfg: B.cascade_paged_config) -> int:
+        return B.cascade_paged_workspace_bytes(cfg) + 256      # the workspace begins at a multiple of 256
 
     def close(self):
         if getattr(self, "ctx", None):

@@ -5,6 +5,7 @@ import numpy as np
 import pytest
 import torch
 
+from paper_2406_17808_amd import binding as B
 from paper_2406_17808_amd import paged
 from test_gpu_paged import DEV, Run, attend_case, i32
 
@@ -161,3 +162,66 @@ def test_two_caches_on_two_streams_and_two_graphs_of_one_cache():
         graphs[0].replay()
         torch.cuda.synchronize()
         assert torch.equal(outs[0], out) and torch.equal(outs[1], want2)
+
+
+def test_layers_on_one_workspace():
+    """Two layers, other head counts and types, on one workspace: eager and captured, what each gives alone."""
+    runs = [attend_case("bf16", 128, 8, 2, 64, [3000, 900], [1, 1], seed=1), attend_case("f32", 64, 4, 1, 32, [700, 2000], [3, 40], seed=2)]
+    size = max(paged.PagedKVCache.workspace_size(run.cfg) for run, _, _, _ in runs)
+    workspace = torch.empty(size, dtype=torch.uint8, device=DEV)
+    layers = [paged.PagedKVCache(run.cfg, DEV, pages=run.cache.pages, workspace=workspace) for run, _, _, _ in runs]
+    for _ in range(2):
+        for layer, (run, batch, q, out) in zip(layers, runs):
+            assert torch.equal(layer.attend(batch, q), out)
+    stream = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=stream):
+        outs = [layer.attend(batch, q) for layer, (run, batch, q, out) in zip(layers, runs)]
+    for _ in range(3):
+        for x in outs:
+            x.zero_()
+        layers[0].attend(runs[0][1], runs[0][2])
+        graph.replay()
+        torch.cuda.synchronize()
+        for x, (run, batch, q, out) in zip(outs, runs):
+            assert torch.equal(x, out)
+    with pytest.raises(AssertionError):
+        paged.PagedKVCache(runs[0][0].cfg, DEV, pages=runs[0][0].cache.pages, workspace=workspace[:1000])
+    with pytest.raises(AssertionError):
+        paged.PagedKVCache(runs[0][0].cfg, DEV, pages=runs[0][0].cache.pages, workspace=workspace.to(torch.int8))
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("hq,hkv,lengths,new,empty", [
+    (300, 1, [100], [3], 0),
+    (1024, 1, [40, 700], [2, 1], 0),
+    (512, 2, [90, 0], [9, 3], 300),
+])
+def test_many_heads_of_a_group(dtype, hq, hkv, lengths, new, empty):
+    """More query heads of a KV head than a workgroup has rows."""
+    run, batch, q, out = attend_case(dtype, 64, hq, hkv, 32, lengths + [0] * empty, new + [0] * empty, seed=hq)
+    run.check_attend(batch, q, out)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("new,empty", [(1, 0), (40, 0), (300, 300)])
+def test_pages_behind_four_gigabytes(dtype, new, empty):
+    """Pages at the end of a pool of more than 2^33 bytes hold and give what the same pages of a small pool do."""
+    lengths, counts = [500] + [0] * empty, [new] + [0] * empty
+    run, batch, q, out = attend_case(dtype, 128, 4, 2, 64, lengths, counts, seed=new)
+    n = (1 << 33) // B.cascade_paged_page_bytes(run.cfg) + 1000
+    cfg = B.make_paged_config(n_q_heads=4, n_kv_heads=2, head_dim=128, dtype=run.cfg.dtype, page_size=64, n_pages=n, max_seqs=len(lengths))
+    cache = paged.PagedKVCache(cfg, DEV)
+    few = run.cache.pages.shape[0]
+    cache.pages[n - few:] = run.cache.pages
+    table = np.where(run.table >= 0, run.table + (n - few), -1)
+    there = paged.PagedBatch(batch.lengths, batch.new_offsets, i32(table), batch.n_tokens, batch.max_new, batch.max_length)
+    assert torch.equal(cache.attend(there, q), out)
+    k, v = run.rows(new, 2), run.rows(new, 2)
+    run.cache.append(batch, k, v)
+    cache.append(there, k, v)
+    assert torch.equal(cache.pages[n - few:], run.cache.pages)
+    for x, y in zip(cache.read(there), run.cache.read(batch)):
+        assert torch.equal(x, y)
+    cache.close()
