@@ -80,7 +80,7 @@ template <typename T> __global__ __launch_bounds__(256) void norm_rope_any_kerne
 }
 
 // Bound by memory: 4096 tokens of 32 + 8 heads, d 128, bf16 (84 MB) take 18.0 us in a row of calls, 4.66 TB/s; a large copy reaches 4.74.  One token takes the device 3.3 us and
-// the caller 12.  (A wave per row with the cosines made for every row, as above: 65 us.)
+// the caller 10.  (A wave per row with the cosines made for every row, as above: 65 us.)
 // Rows of whole 16-byte pieces, TPR threads a row (the first d / 16 of them work), each with 8 channels of the lower half and their partners of
 // the upper half: the rotation needs no exchange.  A workgroup has all rows of `per` tokens (or, with more than 1024 / TPR rows a token, goes over
 // them), whose cosines and sines are made once, in LDS, while the rows are on their way.

@@ -18,6 +18,14 @@ _TYPES = {torch.bfloat16: B.CASCADE_BF16, torch.float32: B.CASCADE_F32}
 _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
 
 
+_current_device = getattr(torch._C, "_cuda_getDevice", torch.cuda.current_device)
+
+
+def _like(x: torch.Tensor) -> torch.Tensor:
+    """A contiguous array of x's shape (half the host time of torch.empty with all of its arguments)."""
+    return torch.empty_like(x, memory_format=torch.contiguous_format)
+
+
 def _stream(device: torch.device) -> int:
     if _raw_stream is not None and device.index is not None:
         return _raw_stream(device.index)
@@ -59,15 +67,18 @@ def qk_norm_rope(q: torch.Tensor, k: Optional[torch.Tensor] = None, q_weight: Op
     of q and k may lie apart (views of a fused projection).  q_out / k_out may be q / k."""
     device, dtype, (tokens, hq, d) = q.device, q.dtype, q.shape
     assert q.is_cuda and dtype in _TYPES, (device, dtype)
+    q_stride, q_out_stride, hk, k_stride, k_out_stride = _rows(q, device, dtype, tokens, hq, d), 0, 0, 0, 0
     if q_out is None:
-        q_out = torch.empty((tokens, hq, d), dtype=dtype, device=device)
-    q_stride, q_out_stride = _rows(q, device, dtype, tokens, hq, d), _rows(q_out, device, dtype, tokens, hq, d)
-    hk = k_stride = k_out_stride = 0
+        q_out = _like(q)
+    else:
+        q_out_stride = _rows(q_out, device, dtype, tokens, hq, d)
     if k is not None:
         hk = k.shape[1]
+        k_stride = _rows(k, device, dtype, tokens, hk, d)
         if k_out is None:
-            k_out = torch.empty((tokens, hk, d), dtype=dtype, device=device)
-        k_stride, k_out_stride = _rows(k, device, dtype, tokens, hk, d), _rows(k_out, device, dtype, tokens, hk, d)
+            k_out = _like(k)
+        else:
+            k_out_stride = _rows(k_out, device, dtype, tokens, hk, d)
     else:
         assert k_out is None and k_weight is None
     for w in (q_weight, k_weight):
@@ -79,7 +90,7 @@ def qk_norm_rope(q: torch.Tensor, k: Optional[torch.Tensor] = None, q_weight: Op
         _TYPES[dtype], d, tokens, hq, hk, norm, eps, 0, q.data_ptr(), k.data_ptr() if hk else None, q_out.data_ptr(), k_out.data_ptr() if hk else None,
         q_stride, k_stride, q_out_stride, k_out_stride, None if q_weight is None else q_weight.data_ptr(), None if k_weight is None else k_weight.data_ptr(),
         *((None, None, 0) if positions is None else (positions.data_ptr(), rope.table.data_ptr(), rope.n_positions)))
-    if torch.cuda.current_device() == device.index:
+    if _current_device() == device.index:
         B.cascade_norm_rope(args, _stream(device))
     else:
         with torch.cuda.device(device):
@@ -163,7 +174,7 @@ class PagedKVCache:
             return None
         q_stride = _rows(q, device, dtype, n, self.n_q_heads, d)
         if q_out is None:
-            q_out = torch.empty((n, self.n_q_heads, d), dtype=dtype, device=device)
+            q_out = _like(q)
         else:
             _rows(q_out, device, dtype, n, self.n_q_heads, d)
             assert q_out.is_contiguous()
@@ -176,7 +187,7 @@ class PagedKVCache:
         assert batch.device == device
         q_stride = _rows(q, device, dtype, n, self.n_q_heads, d)
         if out is None:
-            out = torch.empty((n, self.n_q_heads, d), dtype=dtype, device=device)
+            out = _like(q)
         else:
             _rows(out, device, dtype, n, self.n_q_heads, d)
             assert out.is_contiguous()
@@ -186,6 +197,7 @@ class PagedKVCache:
     def read(self, batch: PagedBatch) -> Tuple[torch.Tensor, torch.Tensor]:
         """The rows that the batch calls new, as the values their codes stand for."""
         assert batch.device == self.device
-        k, v = (torch.empty((batch.n_tokens, self.n_kv_heads, self.head_dim), dtype=self.torch_dtype, device=self.device) for _ in range(2))
+        k = torch.empty((batch.n_tokens, self.n_kv_heads, self.head_dim), dtype=self.torch_dtype, device=self.device)
+        v = _like(k)
         B.cascade_paged_read(self.ctx, batch.c, k.data_ptr(), v.data_ptr(), _stream(self.device))
         return k, v
