@@ -454,6 +454,7 @@ void cascade_paged_destroy(cascade_paged_ctx* ctx);
  *   dev_q if that is contiguous); needs the table.
  * attend: dev_out[t] = softmax attention of query t (already rotated) over its sequence's positions up to its own (within the window).
  *   The new tokens' keys have to be in the cache (append).  A query that sees nothing gives zeros.
+ *   Logits below the range of 32 bits are -infinity: such keys have no weight next to others, and a query that sees no other key gives NaN.
  * read: the new tokens' rows as the values they stand for, into contiguous dev_k_out and dev_v_out (either may be NULL); a row that was left out
  *   on writing (see cascade_paged_batch) is read as zeros.  Any range of a sequence can be read by a batch that calls it new.
  */

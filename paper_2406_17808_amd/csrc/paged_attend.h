@@ -50,6 +50,26 @@ __device__ inline KeySpan key_span(const PagedGeom& g, const PagedBatch& b, cons
     return k;
 }
 
+// What the running maximum of a row (in units of log2) begins with: finite, so that a row that has seen nothing, or only logits of -infinity, gets exponentials of 0
+// and factors of 1 without a test.
+constexpr float kNoLogit = -3.4028234663852886e38f;
+
+// Whether the query at `pos` sees a key that exists in groups [first, last): what tells a row of logits of -infinity, whose softmax is NaN, from a row without keys, which
+// gives zeros.
+__device__ inline bool sees_a_key(const PagedGeom& g, const PagedBatch& b, int s, int pos, int first, int last)
+{
+    const int from = max(first * kGroupTokens, g.window ? pos - g.window + 1 : 0), to = min(last * kGroupTokens, min(pos + 1, b.max_length));
+    for (int p = from; p < to; p = (p / kGroupTokens + 1) * kGroupTokens)
+        if (paged_group(g, b, s, p) >= 0) return true;
+    return false;
+}
+
+// One over the sum of a row's probabilities.  Where there is no logit, all of them are 0 and `total` counts the parts of the row that see a key (or is NaN).
+__device__ inline float row_factor(float top, float total)
+{
+    return top != kNoLogit ? 1.f / total : total == 0.f ? 0.f : __uint_as_float(0x7FC00000u);
+}
+
 // The larger of two numbers, NaN if one is: an instruction of its own on gfx950 (fmaxf first makes its operands canonical, one instruction each).
 __device__ inline float max_of(float a, float b) { return __builtin_elementwise_maximum(a, b); }
 

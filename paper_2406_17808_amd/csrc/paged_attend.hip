@@ -133,9 +133,11 @@ template <typename T, int D, int NT> __global__ __launch_bounds__(kFewWaves * 64
 
     f32x4_t o[NT][D / 16];
     float top[NT], sum[NT];      // running maximum (in units of log2) and the lane's part of the row sum
+    bool saw_whole = false, saw[NT];      // whether a group that every column sees whole, or a key that the lane's column sees, was there
 #pragma unroll
     for (int n = 0; n < NT; ++n) {
-        top[n] = -INFINITY;
+        top[n] = kNoLogit;
+        saw[n] = false;
         sum[n] = 0.f;
 #pragma unroll
         for (int t = 0; t < D / 16; ++t) o[n][t] = f32x4_t{0.f, 0.f, 0.f, 0.f};
@@ -197,6 +199,7 @@ template <typename T, int D, int NT> __global__ __launch_bounds__(kFewWaves * 64
                             const int key = key0 + 16 * (j >> 2) + 4 * qq + (j & 3);
                             seen[j] = key >= from && key < to;
                             if (!seen[j]) st[n][j >> 2][j & 3] = -INFINITY;
+                            saw[n] |= seen[j];
                         }
                     }
                     float mx = st[n][0][0];
@@ -205,7 +208,7 @@ template <typename T, int D, int NT> __global__ __launch_bounds__(kFewWaves * 64
                     mx *= scale;
                     if (__ballot(mx > top[n] + kRescaleLog2)) {
                         const float now = max_of(top[n], max_quarters(mx));
-                        const float shrink = now == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(top[n] - now);
+                        const float shrink = __builtin_amdgcn_exp2f(top[n] - now);
                         top[n] = now;
                         sum[n] *= shrink;
 #pragma unroll
@@ -214,8 +217,7 @@ template <typename T, int D, int NT> __global__ __launch_bounds__(kFewWaves * 64
                     float p[8];
 #pragma unroll
                     for (int j = 0; j < 8; ++j) {
-                        float e = __builtin_amdgcn_exp2f(__builtin_fmaf(st[n][j >> 2][j & 3], scale, -top[n]));
-                        if (decltype(some)::value) e = seen[j] ? e : 0.f;
+                        const float e = __builtin_amdgcn_exp2f(__builtin_fmaf(st[n][j >> 2][j & 3], scale, -top[n]));
                         sum[n] += e;
                         const uint32_t w = cur.scales[j >> 1];
                         p[j] = e * __uint_as_float(j & 1 ? w & 0xFFFF0000u : w << 16);
@@ -228,6 +230,7 @@ template <typename T, int D, int NT> __global__ __launch_bounds__(kFewWaves * 64
                     }
                 }
             };
+            saw_whole |= whole;
             if (whole) probabilities(std::false_type());
             else probabilities(std::true_type());
 #pragma unroll
@@ -253,7 +256,7 @@ template <typename T, int D, int NT> __global__ __launch_bounds__(kFewWaves * 64
 #pragma unroll
     for (int n = 0; n < NT; ++n) {
         if (n) __syncthreads();
-        const float whole_sum = sum_quarters(sum[n]);
+        const float whole_sum = sum_quarters(top[n] == kNoLogit && (saw_whole || saw[n]) ? sum[n] + 1.f : sum[n]);      // (row_factor)
         if (qq == 0) {
             m_wave[wave][m] = top[n];
             l_wave[wave][m] = whole_sum;
@@ -270,7 +273,7 @@ template <typename T, int D, int NT> __global__ __launch_bounds__(kFewWaves * 64
             float l = 0.f, x[kEach] = {};
 #pragma unroll
             for (int w = 0; w < kFewWaves; ++w) {
-                const float f = m_wave[w][c] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m_wave[w][c] - all);
+                const float f = __builtin_amdgcn_exp2f(m_wave[w][c] - all);
                 l += f * l_wave[w][c];
 #pragma unroll
                 for (int e = 0; e < kEach; ++e) x[e] += f * o_wave[w][c][at + e];
@@ -278,7 +281,7 @@ template <typename T, int D, int NT> __global__ __launch_bounds__(kFewWaves * 64
             const int i = row / g.G, h = row - i * g.G;
             if (alone) {
                 T* y = out + ((int64_t)(v.first + i) * g.Hq + hk * g.G + h) * D + at;
-                const float r = all == -INFINITY ? 0.f : 1.f / l;
+                const float r = row_factor(all, l);
 #pragma unroll
                 for (int e = 0; e < kEach; e += 4) store4(y + e, x[e] * r, x[e + 1] * r, x[e + 2] * r, x[e + 3] * r);
             } else {
@@ -306,7 +309,7 @@ template <typename T, int D> __global__ __launch_bounds__(256) void merge_few_ke
     // what a launch of plan.splits may hold is on its way before the sequence is looked up: one token on 131072 keys 33.4 -> 32.3 us, on 16384 11.6 -> 11.2
     float2 ml[2];      // of at most kFewMaxSplits, two a thread
 #pragma unroll
-    for (int i = 0; i < 2; ++i) ml[i] = tid + 256 * i < plan.splits ? *(const float2*)(x + (tid + 256 * i) * step + D) : make_float2(-INFINITY, 0.f);
+    for (int i = 0; i < 2; ++i) ml[i] = tid + 256 * i < plan.splits ? *(const float2*)(x + (tid + 256 * i) * step + D) : make_float2(kNoLogit, 0.f);
     float2 first[kFirst][2];
 #pragma unroll
     for (int n = 0; n < kFirst; ++n) {
@@ -323,7 +326,7 @@ template <typename T, int D> __global__ __launch_bounds__(256) void merge_few_ke
     if (splits <= 1) return;      // written by its only split
 #pragma unroll
     for (int i = 0; i < 2; ++i)
-        if (tid + 256 * i >= splits) ml[i] = make_float2(-INFINITY, 0.f);
+        if (tid + 256 * i >= splits) ml[i] = make_float2(kNoLogit, 0.f);
     float top = fmaxf(ml[0].x, ml[1].x);
 #pragma unroll
     for (int w = 32; w; w >>= 1) top = fmaxf(top, __shfl_xor(top, w));
@@ -333,7 +336,7 @@ template <typename T, int D> __global__ __launch_bounds__(256) void merge_few_ke
     float l = 0.f;
 #pragma unroll
     for (int i = 0; i < 2; ++i) {
-        const float f = ml[i].x == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(ml[i].x - top);
+        const float f = __builtin_amdgcn_exp2f(ml[i].x - top);
         weight[tid + 256 * i] = f;
         l += f * ml[i].y;
     }
@@ -364,7 +367,7 @@ template <typename T, int D> __global__ __launch_bounds__(256) void merge_few_ke
         for (int i = 0; i < kParts; ++i) o[e] += o_part[i][c + e];
     }
     const int i = row / g.G, h = row - i * g.G;
-    const float r = top == -INFINITY ? 0.f : 1.f / l;
+    const float r = row_factor(top, l);
     store4(out + ((int64_t)(v.first + i) * g.Hq + hk * g.G + h) * D + c, o[0] * r, o[1] * r, o[2] * r, o[3] * r);
 }
 
@@ -381,14 +384,14 @@ template <typename T, int D> __global__ __launch_bounds__(256) void merge_rows_k
     if (splits <= 1) return;
     const float* x = part + ((int64_t)(s * g.Hkv + hk) * plan.splits * plan.max_rows + row) * (D + 2);
     const int64_t step = (int64_t)plan.max_rows * (D + 2);
-    float top = -INFINITY;
+    float top = kNoLogit;
 #pragma unroll 4
     for (int i = 0; i < splits; ++i) top = fmaxf(top, x[i * step + D]);
     float l = 0.f, o[4] = {};
 #pragma unroll 4
     for (int i = 0; i < splits; ++i) {
         const float2 a = *(const float2*)(x + i * step + c), e = *(const float2*)(x + i * step + c + 2), ml = *(const float2*)(x + i * step + D);
-        const float f = ml.x == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(ml.x - top);
+        const float f = __builtin_amdgcn_exp2f(ml.x - top);
         l += f * ml.y;
         o[0] += f * a.x;
         o[1] += f * a.y;
@@ -396,7 +399,7 @@ template <typename T, int D> __global__ __launch_bounds__(256) void merge_rows_k
         o[3] += f * e.y;
     }
     const int i = row / g.G, h = row - i * g.G;
-    const float r = top == -INFINITY ? 0.f : 1.f / l;
+    const float r = row_factor(top, l);
     store4(out + ((int64_t)(v.first + i) * g.Hq + hk * g.G + h) * D + c, o[0] * r, o[1] * r, o[2] * r, o[3] * r);
 }
 

@@ -54,6 +54,7 @@ template <typename T, int D, int NW> __global__ __launch_bounds__(NW * 64, 1) vo
     __shared__ __attribute__((aligned(16))) bf16_t k_lds[2][kBN * D], v_lds[2][kBN * D];
     __shared__ __attribute__((aligned(16))) float vs_lds[2][kBN];
     __shared__ uint32_t special_lds;
+    __shared__ float sees_lds[kRows];      // 1: the row sees a key of this range
     __shared__ uint32_t odd_lds[2][2], gone_lds[2][2];      // of a group: bits of V slots whose scale is an infinity or NaN; whether the group is missing
 
     const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), l = tid & 63, l32 = l & 31, half = l >> 5;
@@ -149,7 +150,7 @@ template <typename T, int D, int NW> __global__ __launch_bounds__(NW * 64, 1) vo
     for (int kb = 0; kb < 2; ++kb)
 #pragma unroll
         for (int j = 0; j < 16; ++j) st[kb][j] = 0.f;
-    float top = -INFINITY, sum = 0.f;
+    float top = kNoLogit, sum = 0.f;
     const float scale = g.scale * 1.44269504088896341f;
 
     // Whether anything in the range needs the careful form of a tile: a group that is missing (looked for here), a V row of NaN (seen when it is
@@ -162,6 +163,11 @@ template <typename T, int D, int NW> __global__ __launch_bounds__(NW * 64, 1) vo
     for (int i = 128 + tid; i < 2 * NT; i += NW * 64) missing |= absent(i, paged_group(g, b, s, (2 * tile0 + i) * kGroupTokens) >= 0);
     missing = __syncthreads_or(missing);
     if (tid == 0) special_lds = missing;
+    {      // kept until the end, where a row without a logit asks for it
+        bool sees = max(from, tile0 * kBN) < min(to, tile1 * kBN);
+        if (missing && sees) sees = sees_a_key(g, b, s, pos, 2 * tile0, 2 * tile1);
+        sees_lds[wave * 32 + l32] = sees ? 1.f : 0.f;
+    }
 
     // (what no row sees is masked anyway, and the fast form leaves gone_lds as it is)
     auto is_gone = [&](int i, auto plain) { return !decltype(plain)::value && missing && held[i].gone; };
@@ -303,7 +309,7 @@ template <typename T, int D, int NW> __global__ __launch_bounds__(NW * 64, 1) vo
         mx *= scale;
         if (__ballot(mx > top + kRescaleLog2)) {
             const float now = max_of(top, max_xor32(mx));
-            const float shrink = now == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(top - now);
+            const float shrink = __builtin_amdgcn_exp2f(top - now);
             top = now;
             sum *= shrink;
 #pragma unroll
@@ -311,11 +317,10 @@ template <typename T, int D, int NW> __global__ __launch_bounds__(NW * 64, 1) vo
 #pragma unroll
                 for (int j = 0; j < 16; ++j) o[db][j] *= shrink;
         }
-        const float ref = top == -INFINITY ? 0.f : top;      // a row that has seen nothing: every exponential is 0
 #pragma unroll
         for (int kb = 0; kb < 2; ++kb)
 #pragma unroll
-            for (int j = 0; j < 16; ++j) st[kb][j] = __builtin_amdgcn_exp2f(__builtin_fmaf(st[kb][j], scale, -ref));
+            for (int j = 0; j < 16; ++j) st[kb][j] = __builtin_amdgcn_exp2f(__builtin_fmaf(st[kb][j], scale, -top));
     };
 
     // ---- the tiles
@@ -376,12 +381,13 @@ template <typename T, int D, int NW> __global__ __launch_bounds__(NW * 64, 1) vo
 
     // ---- rows out: lane l has channels 32 db + 8 (j / 4) + 4 half + j % 4 of its row
     const auto both = __builtin_amdgcn_permlane32_swap(__float_as_uint(sum), __float_as_uint(sum), false, false);
-    const float total = __uint_as_float(both[0]) + __uint_as_float(both[1]);
+    float total = __uint_as_float(both[0]) + __uint_as_float(both[1]);
     if (row >= rows) return;
+    if (total == 0.f) total = sees_lds[wave * 32 + l32];      // (row_factor)
     if (plan.splits == 1) {
         const int i = row / g.G, h = row - i * g.G;
         T* y = out + ((int64_t)(v.first + i) * g.Hq + hk * g.G + h) * D + 4 * half;
-        const float r = total == 0.f ? 0.f : 1.f / total;
+        const float r = row_factor(top, total);
 #pragma unroll
         for (int db = 0; db < DB; ++db)
 #pragma unroll
@@ -409,11 +415,11 @@ template <typename T, int D> __global__ __launch_bounds__(256) void merge_chunk_
     if (row >= v.n * g.G) return;
     const float* x = part + ((int64_t)(unit * g.Hkv + hk) * plan.splits * block_rows + in_block) * (D + 2);
     const int64_t step = (int64_t)block_rows * (D + 2);
-    float top = -INFINITY;
+    float top = kNoLogit;
     for (int i = 0; i < plan.splits; ++i) top = fmaxf(top, x[i * step + D]);
     float l = 0.f, o[4] = {};
     for (int i = 0; i < plan.splits; ++i) {
-        const float m = x[i * step + D], f = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m - top);
+        const float m = x[i * step + D], f = __builtin_amdgcn_exp2f(m - top);
         const float2 a = *(const float2*)(x + i * step + c), e = *(const float2*)(x + i * step + c + 2);
         l += f * x[i * step + D + 1];
         o[0] += f * a.x;
@@ -422,7 +428,7 @@ template <typename T, int D> __global__ __launch_bounds__(256) void merge_chunk_
         o[3] += f * e.y;
     }
     const int i = row / g.G, h = row - i * g.G;
-    const float r = l == 0.f ? 0.f : 1.f / l;
+    const float r = row_factor(top, l);
     store4(out + ((int64_t)(v.first + i) * g.Hq + hk * g.G + h) * D + c, o[0] * r, o[1] * r, o[2] * r, o[3] * r);
 }
 
