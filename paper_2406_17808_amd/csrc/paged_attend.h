@@ -54,6 +54,12 @@ __device__ inline KeySpan key_span(const PagedGeom& g, const PagedBatch& b, cons
 // and factors of 1 without a test.
 constexpr float kNoLogit = -3.4028234663852886e38f;
 
+// An exponential of fma(logit, scale, -maximum) is off by what the maximum was rounded by, the same for all keys of a row: nothing for ordinary logits, a factor of up to 2
+// where the maximum (in units of log2) is 2^24, an overflow from 2^31 on.  A wave that has come by a maximum of this size rounds its products with the scale before
+// it subtracts.
+constexpr float kFarLogit = 16777216.f;
+__device__ inline bool is_far(float top) { return fabsf(top) >= kFarLogit && top != kNoLogit; }
+
 // Whether the query at `pos` sees a key that exists in groups [first, last): what tells a row of logits of -infinity, whose softmax is NaN, from a row without keys, which
 // gives zeros.
 __device__ inline bool sees_a_key(const PagedGeom& g, const PagedBatch& b, int s, int pos, int first, int last)

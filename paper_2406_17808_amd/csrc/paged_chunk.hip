@@ -150,6 +150,7 @@ template <typename T, int D, int NW> __global__ __launch_bounds__(NW * 64, 1) vo
     for (int kb = 0; kb < 2; ++kb)
 #pragma unroll
         for (int j = 0; j < 16; ++j) st[kb][j] = 0.f;
+    bool far = false;      // a row of the wave has come by a maximum of kFarLogit
     float top = kNoLogit, sum = 0.f;
     const float scale = g.scale * 1.44269504088896341f;
 
@@ -309,6 +310,7 @@ template <typename T, int D, int NW> __global__ __launch_bounds__(NW * 64, 1) vo
         mx *= scale;
         if (__ballot(mx > top + kRescaleLog2)) {
             const float now = max_of(top, max_xor32(mx));
+            far |= __ballot(is_far(now)) != 0;
             const float shrink = __builtin_amdgcn_exp2f(top - now);
             top = now;
             sum *= shrink;
@@ -317,10 +319,16 @@ template <typename T, int D, int NW> __global__ __launch_bounds__(NW * 64, 1) vo
 #pragma unroll
                 for (int j = 0; j < 16; ++j) o[db][j] *= shrink;
         }
+        if (__builtin_expect(far, 0))
+#pragma unroll
+            for (int kb = 0; kb < 2; ++kb)
+#pragma unroll
+                for (int j = 0; j < 16; ++j) st[kb][j] *= scale;
+        const float unit = far ? 1.f : scale;
 #pragma unroll
         for (int kb = 0; kb < 2; ++kb)
 #pragma unroll
-            for (int j = 0; j < 16; ++j) st[kb][j] = __builtin_amdgcn_exp2f(__builtin_fmaf(st[kb][j], scale, -top));
+            for (int j = 0; j < 16; ++j) st[kb][j] = __builtin_amdgcn_exp2f(__builtin_fmaf(st[kb][j], unit, -top));
     };
 
     // ---- the tiles

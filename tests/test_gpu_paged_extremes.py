@@ -107,3 +107,41 @@ def test_all_logits_minus_infinity_or_no_keys(call, dtype):
     run, batch, q, out = made(call, dtype, 64, lambda s, p: True, -(2.0 ** 40), 2.0 ** 100, seed=4, missing=missing)
     counted = check_without(run, q, out, lambda s, p: True)
     assert counted["zero"] == new[0] * hkv and counted["nan"] == sum(new[1:]) * hkv
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("call", CALLS)
+@pytest.mark.parametrize("exponent", [20, 27, 31, 45, 100])
+def test_large_finite_logits(call, dtype, d, exponent):
+    """Logits of 2^20 to 2^100 in size, above and below zero: the keys with the largest share the row, whatever a product with the scale rounds to."""
+    g, hkv, lengths, new, empty = CALLS[call]
+    lengths, new = lengths + [0] * empty, new + [0] * empty
+    rng = np.random.default_rng(exponent + d)
+    table, n_pages = pages_for(rng, lengths, new, 32)
+    run = Run(dtype, d, g * hkv, hkv, 32, n_pages, len(lengths), seed=exponent, fill=0xFF)
+    total = [a + b for a, b in zip(lengths, new)]
+    size = torch.from_numpy(rng.choice([1.0, 1.5, 2.0, 3.0, 4.0, 6.0], sum(total))).to("cuda:0")      # (no channel but one: the logits are exact)
+    k, v = torch.zeros_like(run.rows(sum(total), hkv)), run.rows(sum(total), hkv)
+    k[..., 0] = size[:, None].to(run.ty)
+    run.cache.append(run.batch([0] * len(total), total, table), k, v)
+    batch = run.batch(lengths, new, table)
+    run.want = run.cache.pages.cpu().numpy()
+    q = run.rows(sum(new), g * hkv)
+    q[..., 0] = 1.37 * 2.0 ** exponent
+    q[:, ::2, 0] *= -1      # (half of the heads: all logits far below zero)
+    out = f64(run.cache.attend(batch, q))
+    for s in range(len(lengths)):
+        a, e = run.offsets[s], run.offsets[s + 1]
+        if a == e:
+            continue
+        n = total[s]
+        seen = np.arange(n)[None] <= (lengths[s] + np.arange(e - a))[:, None]
+        for h in range(hkv):
+            kv, vv, _ = run.values(s, h, n)
+            for x in range(g):
+                rows = f64(q)[a:e, h * g + x].copy()
+                rows[:, 1:] = 0
+                want, weighted, _ = M.attend(rows, kv, vv, seen, run.scale)      # differences of the logits: none, or above 2^16
+                tol = M.attend_tolerance(run.ty, want, weighted, np.zeros(e - a), d, n)
+                assert (np.abs(out[a:e, h * g + x] - want) <= tol).all(), (s, h, x)
