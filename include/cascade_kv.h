@@ -328,14 +328,14 @@ const char* cascade_last_error(const cascade_ctx* ctx);
  * Rotation table: cosines and sines of p * theta_i, theta_i = base^(-2i/d), for positions
  * 0 <= p < n_positions, as two tables in 64 bits (every 256th position, and 256 offsets) whose
  * entries are combined by the angle sum: 4.5 MB for a million positions at head_dim 128, exact to the
- * last bits of a float.  The buffer is the caller's, 16-byte aligned, and may be shared by all calls that
+ * last bits of a float.  The base is a 64-bit number: one rounded to 32 bits turns position 10^5 by up to 2e-4 too far.  The buffer is the caller's, 16-byte aligned, and may be shared by all calls that
  * take dev_rope, on any number of contexts.
  *   cascade_rope_table_bytes: size of the buffer; 0 for arguments out of range (head_dim even and 2 to 256,
  *     1 <= n_positions <= 2^31).
  * Errors: NULL_ARG, BAD_ARG (range, alignment, base not above 0), WORKSPACE_TOO_SMALL, HIP.
  */
 size_t cascade_rope_table_bytes(int64_t n_positions, int32_t head_dim);
-int cascade_rope_table(void* dev_rope, size_t bytes, int64_t n_positions, int32_t head_dim, float base, void* stream);
+int cascade_rope_table(void* dev_rope, size_t bytes, int64_t n_positions, int32_t head_dim, double base, void* stream);
 
 /*
  * Per-head RMS norm of queries and keys with the rotation in the same pass, for every row x of head_dim values:

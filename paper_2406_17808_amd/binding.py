@@ -179,7 +179,7 @@ def load_library():
         L.cascade_rope_table_bytes.restype = ctypes.c_size_t
         L.cascade_rope_table_bytes.argtypes = [I64, ctypes.c_int32]
         L.cascade_rope_table.restype = ctypes.c_int
-        L.cascade_rope_table.argtypes = [P, ctypes.c_size_t, I64, ctypes.c_int32, ctypes.c_float, P]
+        L.cascade_rope_table.argtypes = [P, ctypes.c_size_t, I64, ctypes.c_int32, ctypes.c_double, P]
         L.cascade_norm_rope.restype = ctypes.c_int
         L.cascade_norm_rope.argtypes = [ctypes.POINTER(cascade_norm_rope_args), P]
         for name in ("cascade_paged_page_bytes", "cascade_paged_workspace_bytes"):

@@ -108,15 +108,15 @@ static int fail_without_context(int code, const char* text)
 }
 #define CKV_REFUSE(code, text) return fail_without_context(code, text)
 
-extern "C" int cascade_rope_table(void* dev_rope, size_t bytes, int64_t n_positions, int32_t head_dim, float base, void* stream)
+extern "C" int cascade_rope_table(void* dev_rope, size_t bytes, int64_t n_positions, int32_t head_dim, double base, void* stream)
 {
     if (!dev_rope) CKV_REFUSE(CASCADE_E_NULL_ARG, "cascade_rope_table: NULL table");
     const size_t need = cascade_rope_table_bytes(n_positions, head_dim);
     if (need == 0) CKV_REFUSE(CASCADE_E_BAD_ARG, "cascade_rope_table: n_positions must be 1 to 2^31, head_dim even and 2 to 256");
-    if (!(base > 0.f) || !isfinite(base)) CKV_REFUSE(CASCADE_E_BAD_ARG, "cascade_rope_table: base must be finite and above 0");
+    if (!(base > 0.0) || !isfinite(base)) CKV_REFUSE(CASCADE_E_BAD_ARG, "cascade_rope_table: base must be finite and above 0");
     if (!aligned(dev_rope, 16)) CKV_REFUSE(CASCADE_E_BAD_ARG, "cascade_rope_table: the table must be 16-byte aligned");
     if (bytes < need) CKV_REFUSE(CASCADE_E_WORKSPACE_TOO_SMALL, "cascade_rope_table: buffer smaller than cascade_rope_table_bytes");
-    launch_rope_pair_table((double2*)dev_rope, n_positions, head_dim, (double)base, (hipStream_t)stream);
+    launch_rope_pair_table((double2*)dev_rope, n_positions, head_dim, base, (hipStream_t)stream);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) CKV_REFUSE(CASCADE_E_HIP, hipGetErrorString(e));
     return CASCADE_OK;
