@@ -142,6 +142,7 @@ class PagedKVCache:
         assert workspace.device == self.device and workspace.dtype == torch.uint8 and workspace.is_contiguous()
         assert workspace.numel() >= self.workspace_size(cfg), "the workspace is smaller than workspace_size(cfg)"
         self.workspace = workspace
+        self._streams = set()
         with torch.cuda.device(self.device):
             self.ctx = B.cascade_paged_init(cfg, pages.data_ptr(), (self.workspace.data_ptr() + 255) & ~255, self.workspace_bytes,
                                             rope.table.data_ptr() if rope is not None else 0, rope.n_positions if rope is not None else 0)
@@ -150,9 +151,21 @@ class PagedKVCache:
     def workspace_size(cfg: B.cascade_paged_config) -> int:
         return B.cascade_paged_workspace_bytes(cfg) + 256      # the workspace begins at a multiple of 256
 
+    def _used_on(self) -> int:
+        """The current stream as a number.  The allocator is told of each that the cache's arrays are used on, so that they are not handed out again before
+        its work is done, whenever the cache is dropped."""
+        stream = _stream(self.device)
+        if stream not in self._streams:
+            now = torch.cuda.current_stream(self.device)
+            for x in (self.pages, self.workspace) + ((self.rope.table,) if self.rope is not None else ()):
+                x.record_stream(now)
+            self._streams.add(stream)
+        return stream
+
     def close(self):
+        """Ends the context, a structure of the host: nothing is waited for, so that a cache may also be collected while a stream is being captured.
+        (A graph that was captured with the cache needs its arrays for as long as it is replayed.)"""
         if getattr(self, "ctx", None):
-            torch.cuda.synchronize(self.device)
             B.cascade_paged_destroy(self.ctx)
             self.ctx = None
 
@@ -170,7 +183,7 @@ class PagedKVCache:
         k_stride, v_stride = _rows(k, device, dtype, n, self.n_kv_heads, d), _rows(v, device, dtype, n, self.n_kv_heads, d)
         if q is None:
             assert q_out is None
-            B.cascade_paged_append(self.ctx, batch.c, k.data_ptr(), k_stride, v.data_ptr(), v_stride, 0, 0, 0, _stream(device))
+            B.cascade_paged_append(self.ctx, batch.c, k.data_ptr(), k_stride, v.data_ptr(), v_stride, 0, 0, 0, self._used_on())
             return None
         q_stride = _rows(q, device, dtype, n, self.n_q_heads, d)
         if q_out is None:
@@ -178,7 +191,7 @@ class PagedKVCache:
         else:
             _rows(q_out, device, dtype, n, self.n_q_heads, d)
             assert q_out.is_contiguous()
-        B.cascade_paged_append(self.ctx, batch.c, k.data_ptr(), k_stride, v.data_ptr(), v_stride, q.data_ptr(), q_stride, q_out.data_ptr(), _stream(device))
+        B.cascade_paged_append(self.ctx, batch.c, k.data_ptr(), k_stride, v.data_ptr(), v_stride, q.data_ptr(), q_stride, q_out.data_ptr(), self._used_on())
         return q_out
 
     def attend(self, batch: PagedBatch, q: torch.Tensor, out: Optional[torch.Tensor] = None) -> torch.Tensor:
@@ -191,7 +204,7 @@ class PagedKVCache:
         else:
             _rows(out, device, dtype, n, self.n_q_heads, d)
             assert out.is_contiguous()
-        B.cascade_paged_attend(self.ctx, batch.c, q.data_ptr(), q_stride, out.data_ptr(), _stream(device))
+        B.cascade_paged_attend(self.ctx, batch.c, q.data_ptr(), q_stride, out.data_ptr(), self._used_on())
         return out
 
     def read(self, batch: PagedBatch) -> Tuple[torch.Tensor, torch.Tensor]:
@@ -199,5 +212,5 @@ class PagedKVCache:
         assert batch.device == self.device
         k = torch.empty((batch.n_tokens, self.n_kv_heads, self.head_dim), dtype=self.torch_dtype, device=self.device)
         v = _like(k)
-        B.cascade_paged_read(self.ctx, batch.c, k.data_ptr(), v.data_ptr(), _stream(self.device))
+        B.cascade_paged_read(self.ctx, batch.c, k.data_ptr(), v.data_ptr(), self._used_on())
         return k, v

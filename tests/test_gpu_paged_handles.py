@@ -1,0 +1,54 @@
+"""Handles of the paged cache on the GPU: dropped while a stream is captured or busy."""
+import gc
+
+import pytest
+import torch
+
+from paper_2406_17808_amd import paged
+from test_gpu_paged import DEV, attend_case
+
+pytestmark = pytest.mark.gpu
+
+
+def test_a_cache_collected_during_a_capture():
+    """Another cache ends while a step is captured: the capture goes on, and its replays give what eager calls give."""
+    run, batch, q, out = attend_case("bf16", 128, 8, 2, 64, [3000, 900], [1, 1], seed=1)
+    dropped, _, _, _ = attend_case("f32", 64, 4, 1, 32, [40], [1], seed=2)
+    got, stream = torch.zeros_like(q), torch.cuda.Stream()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=stream):
+        del dropped
+        gc.collect()
+        run.cache.attend(batch, q, out=got)
+    for _ in range(3):
+        got.zero_()
+        assert torch.equal(run.cache.attend(batch, q), out)
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(got, out)
+
+
+@pytest.mark.parametrize("own_pages", [True, False])
+def test_a_cache_dropped_while_another_stream_still_uses_it(own_pages):
+    """Its arrays are not handed out again before the work of that stream is done."""
+    run, batch, q, out = attend_case("bf16", 128, 8, 2, 64, [700], [1], seed=3)
+    pages = None if own_pages else torch.empty_like(run.cache.pages)
+    cache = paged.PagedKVCache(run.cfg, DEV, pages=pages)
+    cache.pages.copy_(run.cache.pages)
+    rope = paged.RopeTable(1000, 128, 1e4, DEV)
+    rotating = paged.PagedKVCache(run.cfg, DEV, pages=cache.pages, rope=rope, workspace=cache.workspace)
+    side = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    held = {x.data_ptr(): x.numel() for x in (cache.pages, cache.workspace, rope.table)}
+    with torch.cuda.stream(side):
+        torch.cuda._sleep(400_000_000)      # a fifth of a second
+        got = cache.attend(batch, q)
+        rotating.append(batch, run.rows(1, 2), run.rows(1, 2))
+    del cache, rotating, pages, rope
+    others = [torch.full((n,), 0xFF, dtype=torch.uint8, device=DEV) for n in held.values() for _ in range(2)]
+    if side.query():
+        pytest.skip("the stream was done before the arrays were asked for")
+    assert not {x.data_ptr() for x in others} & set(held)
+    side.synchronize()
+    assert torch.equal(got, out)

@@ -1,0 +1,41 @@
+"""The torch layer of the norms and the paged cache without a GPU: handles, devices, bounds and gradients."""
+import gc
+
+import pytest
+import torch
+
+from paper_2406_17808_amd import binding as B
+from paper_2406_17808_amd import paged
+
+
+def cfg(**kw):
+    base = dict(n_q_heads=8, n_kv_heads=2, head_dim=64, dtype=B.CASCADE_BF16, page_size=64, n_pages=10, max_seqs=4)
+    base.update(kw)
+    return B.make_paged_config(**base)
+
+
+@pytest.fixture(scope="module", autouse=True)
+def lib():
+    import os
+    if not os.path.exists(B.library_path()):
+        from paper_2406_17808_amd.build import build_library
+        build_library()
+    return B.load_library()
+
+
+@pytest.mark.parametrize("end", ["close", "delete"])
+def test_ending_a_cache_does_not_wait_for_the_device(monkeypatch, end):
+    """A cache may be collected while a stream is being captured, where a synchronisation is an error that ends the capture; there is nothing to
+    wait for, its context is a structure of the host."""
+    waits = []
+    monkeypatch.setattr(torch.cuda, "synchronize", lambda *a: waits.append(a))
+    monkeypatch.setattr(paged.B, "cascade_paged_destroy", lambda ctx: waits.append("destroyed") if ctx == 7 else None)
+    cache = paged.PagedKVCache.__new__(paged.PagedKVCache)
+    cache.ctx, cache.device = 7, torch.device("cuda", 0)
+    if end == "close":
+        cache.close()
+        assert cache.ctx is None
+    else:
+        del cache
+        gc.collect()
+    assert waits == ["destroyed"]
