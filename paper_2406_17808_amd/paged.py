@@ -26,8 +26,14 @@ def _like(x: torch.Tensor) -> torch.Tensor:
     return torch.empty_like(x, memory_format=torch.contiguous_format)
 
 
+def _numbered(device) -> torch.device:
+    """The device that tensors made on `device` report: "cuda" is the current one."""
+    device = torch.device(device)
+    return torch.device("cuda", _current_device()) if device.type == "cuda" and device.index is None else device
+
+
 def _stream(device: torch.device) -> int:
-    if _raw_stream is not None and device.index is not None:
+    if _raw_stream is not None:
         return _raw_stream(device.index)
     return torch.cuda.current_stream(device).cuda_stream
 
@@ -51,7 +57,7 @@ class RopeTable:
 
     def __init__(self, n_positions: int, head_dim: int, base: float, device: str = "cuda:0"):
         self.n_positions, self.head_dim, self.base = n_positions, head_dim, base
-        self.device = torch.device(device)
+        self.device = _numbered(device)
         nbytes = B.cascade_rope_table_bytes(n_positions, head_dim)
         self.table = torch.empty(max(nbytes, 16), dtype=torch.uint8, device=self.device)
         with torch.cuda.device(self.device):
@@ -126,7 +132,7 @@ class PagedKVCache:
                  workspace: Optional[torch.Tensor] = None):
         self.cfg, self.rope = cfg, rope
         self.n_q_heads, self.n_kv_heads, self.head_dim = cfg.n_q_heads, cfg.n_kv_heads, cfg.head_dim
-        self.device = torch.device(device)
+        self.device = _numbered(device)
         self.torch_dtype = torch.bfloat16 if cfg.dtype == B.CASCADE_BF16 else torch.float32
         self.page_bytes = B.cascade_paged_page_bytes(cfg)
         self.workspace_bytes = B.cascade_paged_workspace_bytes(cfg)

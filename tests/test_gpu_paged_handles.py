@@ -52,3 +52,15 @@ def test_a_cache_dropped_while_another_stream_still_uses_it(own_pages):
     assert not {x.data_ptr() for x in others} & set(held)
     side.synchronize()
     assert torch.equal(got, out)
+
+
+def test_a_device_without_a_number():
+    """"cuda" is the current device, for tables and caches as for tensors."""
+    run, batch, q, out = attend_case("bf16", 64, 4, 2, 32, [40], [3], seed=4)
+    rope = paged.RopeTable(100, 64, 1e4, "cuda")
+    cache = paged.PagedKVCache(run.cfg, "cuda", rope=rope)
+    assert cache.device == cache.pages.device == rope.device == torch.device("cuda", torch.cuda.current_device())
+    cache.pages.copy_(run.cache.pages)
+    assert torch.equal(cache.attend(batch, q), out)
+    paged.qk_norm_rope(q, positions=torch.arange(3, device="cuda", dtype=torch.int32), rope=rope)
+    paged.PagedKVCache(run.cfg, torch.device("cuda"), pages=run.cache.pages).append(batch, q[:, :2], q[:, 2:])

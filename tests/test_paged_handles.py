@@ -39,3 +39,9 @@ def test_ending_a_cache_does_not_wait_for_the_device(monkeypatch, end):
         del cache
         gc.collect()
     assert waits == ["destroyed"]
+
+
+def test_devices_without_a_number_are_the_current_one(monkeypatch):
+    monkeypatch.setattr(paged, "_current_device", lambda: 3)
+    assert paged._numbered("cuda") == torch.device("cuda", 3) == paged._numbered(torch.device("cuda"))
+    assert paged._numbered("cuda:1") == torch.device("cuda", 1) and paged._numbered("cpu") == torch.device("cpu")
