@@ -52,6 +52,13 @@ def _rows(x: torch.Tensor, device, dtype, tokens: int, heads: int, head_dim: int
     return strides[0]
 
 
+def _serving_only(*inputs: Optional[torch.Tensor]) -> None:
+    if torch.is_grad_enabled():
+        for x in inputs:
+            if x is not None and x.requires_grad:
+                raise RuntimeError("norms and the paged cache have no backward pass: call them under torch.no_grad(), or with inputs that require no gradient")
+
+
 class RopeTable:
     """Cosines and sines of the positions below n_positions (pairs (i, i + head_dim / 2), angles p * base^(-2i / head_dim))."""
 
@@ -70,7 +77,8 @@ def qk_norm_rope(q: torch.Tensor, k: Optional[torch.Tensor] = None, q_weight: Op
                  k_out: Optional[torch.Tensor] = None) -> Tuple[torch.Tensor, Optional[torch.Tensor]]:
     """RMS norm over head_dim of q [tokens, q heads, head_dim] and k [tokens, k heads, head_dim] with the rotation to `positions`
     [tokens] (int32; None: not rotated, as CascadeKVCache takes them) in the same pass.  norm=False rotates only.  Tokens
-    of q and k may lie apart (views of a fused projection).  q_out / k_out may be q / k."""
+    of q and k may lie apart (views of a fused projection).  q_out / k_out may be q / k.  For serving: inputs that require a gradient are refused."""
+    _serving_only(q, k, q_weight, k_weight)
     device, dtype, (tokens, hq, d) = q.device, q.dtype, q.shape
     assert q.is_cuda and dtype in _TYPES, (device, dtype)
     q_stride, q_out_stride, hk, k_stride, k_out_stride = _rows(q, device, dtype, tokens, hq, d), 0, 0, 0, 0
@@ -184,6 +192,7 @@ class PagedKVCache:
     def append(self, batch: PagedBatch, k: torch.Tensor, v: torch.Tensor, q: Optional[torch.Tensor] = None,
                q_out: Optional[torch.Tensor] = None) -> Optional[torch.Tensor]:
         """Stores k, v [n_tokens, kv heads, head_dim] of the batch's new tokens; q [n_tokens, q heads, head_dim] is rotated into q_out, which is returned."""
+        _serving_only(k, v, q)
         n, d, device, dtype = batch.n_tokens, self.head_dim, self.device, self.torch_dtype
         assert batch.device == device
         k_stride, v_stride = _rows(k, device, dtype, n, self.n_kv_heads, d), _rows(v, device, dtype, n, self.n_kv_heads, d)
@@ -202,6 +211,7 @@ class PagedKVCache:
 
     def attend(self, batch: PagedBatch, q: torch.Tensor, out: Optional[torch.Tensor] = None) -> torch.Tensor:
         """Attention of q [n_tokens, q heads, head_dim], rotated, over the cache, the batch's new tokens included."""
+        _serving_only(q)
         n, d, device, dtype = batch.n_tokens, self.head_dim, self.device, self.torch_dtype
         assert batch.device == device
         q_stride = _rows(q, device, dtype, n, self.n_q_heads, d)

@@ -64,3 +64,23 @@ def test_a_device_without_a_number():
     assert torch.equal(cache.attend(batch, q), out)
     paged.qk_norm_rope(q, positions=torch.arange(3, device="cuda", dtype=torch.int32), rope=rope)
     paged.PagedKVCache(run.cfg, torch.device("cuda"), pages=run.cache.pages).append(batch, q[:, :2], q[:, 2:])
+
+
+def test_inputs_that_require_gradients_are_refused():
+    run, batch, q, out = attend_case("f32", 64, 4, 2, 32, [40], [3], seed=5)
+    rope = paged.RopeTable(100, 64, 1e4, DEV)
+    rotating = paged.PagedKVCache(run.cfg, DEV, pages=run.cache.pages, rope=rope)
+    k, v, w = run.rows(3, 2), run.rows(3, 2), run.rows(1, 1)[0, 0]
+    leaf = lambda x: x.clone().requires_grad_()  # noqa: E731
+    calls = [lambda: paged.qk_norm_rope(leaf(q)), lambda: paged.qk_norm_rope(q, leaf(k)), lambda: paged.qk_norm_rope(q, q_weight=leaf(w)),
+             lambda: paged.qk_norm_rope(q, k, k_weight=leaf(w)), lambda: rotating.append(batch, leaf(k), v), lambda: rotating.append(batch, k, leaf(v)),
+             lambda: rotating.append(batch, k, v, q=leaf(q)), lambda: rotating.attend(batch, leaf(q))]
+    pages = run.cache.pages.clone()
+    for call in calls:
+        with pytest.raises(RuntimeError, match="backward"):
+            call()
+    assert torch.equal(run.cache.pages, pages)
+    with torch.no_grad():
+        for call in calls:
+            call()
+    assert torch.equal(rotating.attend(batch, leaf(q).detach()), rotating.attend(batch, q))

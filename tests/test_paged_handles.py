@@ -45,3 +45,16 @@ def test_devices_without_a_number_are_the_current_one(monkeypatch):
     monkeypatch.setattr(paged, "_current_device", lambda: 3)
     assert paged._numbered("cuda") == torch.device("cuda", 3) == paged._numbered(torch.device("cuda"))
     assert paged._numbered("cuda:1") == torch.device("cuda", 1) and paged._numbered("cpu") == torch.device("cpu")
+
+
+def test_what_would_need_a_backward_is_refused():
+    """Outputs have no gradient: with inputs that require one they would be cut from the graph without a word."""
+    plain, leaf = torch.zeros(3), torch.zeros(3, requires_grad=True)
+    paged._serving_only(plain, None)
+    for args in ((leaf,), (plain, leaf), (None, plain, leaf * 2)):
+        with pytest.raises(RuntimeError, match="backward"):
+            paged._serving_only(*args)
+        with torch.no_grad():
+            paged._serving_only(*args)
+        with torch.inference_mode():
+            paged._serving_only(*args)
