@@ -396,8 +396,17 @@ def cascade_simulate_structure(cfg: cascade_config, chunk_sizes: Sequence[int],
                        slot[:slots], None, None, swaps)
 
 
+def check_int32(code: int, **fields: int) -> None:
+    """The structures' fields of 32 bits take any whole number and keep its low bits: what does not fit is refused here."""
+    for name, x in fields.items():
+        if not -(1 << 31) <= x < 1 << 31:
+            raise CascadeError(code, f"{name} = {x} does not fit 32 bits")
+
+
 def make_paged_config(n_q_heads: int, n_kv_heads: int, head_dim: int, dtype: int, page_size: int, n_pages: int, max_seqs: int,
                       softmax_scale: float = 0.0, window: int = 0) -> cascade_paged_config:
+    check_int32(CASCADE_E_INVALID_CONFIG, n_q_heads=n_q_heads, n_kv_heads=n_kv_heads, head_dim=head_dim, dtype=dtype, page_size=page_size,
+                max_seqs=max_seqs, window=window)
     return cascade_paged_config(n_q_heads=n_q_heads, n_kv_heads=n_kv_heads, head_dim=head_dim, dtype=dtype, page_size=page_size,
                                 max_seqs=max_seqs, n_pages=n_pages, softmax_scale=softmax_scale, window=window)
 

@@ -80,7 +80,7 @@ def qk_norm_rope(q: torch.Tensor, k: Optional[torch.Tensor] = None, q_weight: Op
     of q and k may lie apart (views of a fused projection).  q_out / k_out may be q / k.  For serving: inputs that require a gradient are refused."""
     _serving_only(q, k, q_weight, k_weight)
     device, dtype, (tokens, hq, d) = q.device, q.dtype, q.shape
-    assert q.is_cuda and dtype in _TYPES, (device, dtype)
+    assert q.is_cuda and dtype in _TYPES and tokens < 1 << 31, (device, dtype, tokens)
     q_stride, q_out_stride, hk, k_stride, k_out_stride = _rows(q, device, dtype, tokens, hq, d), 0, 0, 0, 0
     if q_out is None:
         q_out = _like(q)
@@ -112,6 +112,12 @@ def qk_norm_rope(q: torch.Tensor, k: Optional[torch.Tensor] = None, q_weight: Op
     return q_out, k_out
 
 
+def _batch_bounds(n_tokens: int, max_new: int, max_length: int) -> Tuple[int, int, int]:
+    bounds = int(n_tokens), int(max_new), int(max_length)
+    B.check_int32(B.CASCADE_E_BAD_ARG, n_tokens=bounds[0], max_new=bounds[1], max_length=bounds[2])
+    return bounds
+
+
 class PagedBatch:
     """The sequences of one call (see cascade_paged_batch): lengths [n] tokens before the new ones, new_offsets [n + 1] rows of the new tokens,
     page_table [n, pages], int32 on the device, and the host's bounds on what they hold.  The arrays are read when the kernels run, so a
@@ -125,7 +131,7 @@ class PagedBatch:
         assert page_table.dim() == 2 and page_table.shape[0] == n and page_table.is_contiguous()
         self.device = lengths.device
         self.lengths, self.new_offsets, self.page_table = lengths, new_offsets, page_table
-        self.n_tokens, self.max_new, self.max_length = int(n_tokens), int(max_new), int(max_length)
+        self.n_tokens, self.max_new, self.max_length = _batch_bounds(n_tokens, max_new, max_length)
         self.c = B.cascade_paged_batch(n_seqs=n, n_tokens=self.n_tokens, max_new=self.max_new, max_length=self.max_length,
                                        dev_lengths=lengths.data_ptr(), dev_new_offsets=new_offsets.data_ptr(),
                                        dev_page_table=page_table.data_ptr(), table_stride=page_table.shape[1])

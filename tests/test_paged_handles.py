@@ -58,3 +58,25 @@ def test_what_would_need_a_backward_is_refused():
             paged._serving_only(*args)
         with torch.inference_mode():
             paged._serving_only(*args)
+
+
+FIELDS = dict(n_q_heads=8, n_kv_heads=2, head_dim=64, dtype=1, page_size=64, max_seqs=4, window=0)
+
+
+@pytest.mark.parametrize("field", FIELDS)
+def test_numbers_of_a_configuration_are_not_cut_to_32_bits(field):
+    for beyond in (FIELDS[field] + 2 ** 32, FIELDS[field] - 2 ** 32, 2 ** 31):
+        with pytest.raises(B.CascadeError) as e:
+            cfg(**{field: beyond})
+        assert e.value.code == B.CASCADE_E_INVALID_CONFIG and field in str(e.value)
+
+
+@pytest.mark.parametrize("field", ["n_tokens", "max_new", "max_length"])
+def test_bounds_of_a_batch_are_not_cut_to_32_bits(field):
+    """2^32 + 100 must not become a bound of 100, behind which keys would not be seen."""
+    bounds = dict(n_tokens=6, max_new=4, max_length=100)
+    paged._batch_bounds(**bounds)
+    for beyond in (bounds[field] + 2 ** 32, bounds[field] - 2 ** 32, 2 ** 31):
+        with pytest.raises(B.CascadeError) as e:
+            paged._batch_bounds(**dict(bounds, **{field: beyond}))
+        assert e.value.code == B.CASCADE_E_BAD_ARG and field in str(e.value)
