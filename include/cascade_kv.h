@@ -395,7 +395,7 @@ typedef struct cascade_paged_config {
     int32_t n_q_heads;         /* a multiple of n_kv_heads, at most 1024 */
     int32_t n_kv_heads;
     int32_t head_dim;          /* 64 or 128 */
-    int32_t dtype;             /* CASCADE_F32 or CASCADE_BF16: q, k, v and outputs */
+    int32_t dtype;             /* CASCADE_F32 or CASCADE_BF16: q, k, v and outputs; what attend rounds probabilities to (see there) */
     int32_t page_size;         /* a multiple of 32, at most 65536 */
     int32_t max_seqs;          /* largest n_seqs of a batch, at most 65535 */
     int64_t n_pages;           /* pages in dev_pages, 2^39 bytes at most */
@@ -406,12 +406,12 @@ typedef struct cascade_paged_config {
 /*
  * The sequences of one call.  Sequence s has dev_lengths[s] tokens in the cache and dev_new_offsets[s+1] - dev_new_offsets[s]
  * new ones, which are rows dev_new_offsets[s] ... of the call's token arrays, at positions dev_lengths[s], dev_lengths[s] + 1, ...
- * Position p lies in page dev_page_table[s * table_stride + p / page_size].  All four arrays are read by the kernels when they run (a captured
+ * Position p lies in page dev_page_table[s * table_stride + p / page_size].  All three arrays are read by the kernels when they run (a captured
  * graph sees what they hold at replay); n_tokens, max_new and max_length are what the host knows, and must bound what the arrays hold.
  * What goes beyond them is left out: tokens from row n_tokens on are neither written nor attended from, positions at or above max_length,
  * behind the end of the table or on a page outside [0, n_pages) are neither written nor seen.
  * Two new tokens on the same slot of the same page (a page listed twice): one of them is stored, or parts of both.
- * Limits (BAD_ARG): n_tokens <= 2^20, max_length <= 2^31 - 2^20, and of the workgroups that a call would need,
+ * Limits (BAD_ARG): n_tokens <= 2^20, max_length < 2^31 - 2^20, and of the workgroups that a call would need,
  * (n_tokens / 32 + 2 n_seqs) * n_kv_heads + n_tokens <= 2^22 and n_tokens * n_q_heads / 128 + n_seqs * n_kv_heads <= 2^22.
  * Bounds far above what the arrays hold cost time: splits and kernels are chosen by them (and with them how sums are rounded).
  */
@@ -450,10 +450,13 @@ void cascade_paged_destroy(cascade_paged_ctx* ctx);
  * Errors: NULL_ARG, BAD_ARG, HIP.
  *
  * append: keys (rotated to their positions if the context has a table, which max_length must not pass) and values of the new tokens into the pages.  dev_q (may be NULL):
- *   their queries, rotated in the same launch into dev_q_out [n_tokens, n_q_heads, head_dim], rounded to the element type (dev_q_out may be
+ *   their queries, rotated in 32 bits in the same launch into dev_q_out [n_tokens, n_q_heads, head_dim], rounded once to the element type (dev_q_out may be
  *   dev_q if that is contiguous); needs the table.
  * attend: dev_out[t] = softmax attention of query t (already rotated) over its sequence's positions up to its own (within the window).
- *   The new tokens' keys have to be in the cache (append).  A query that sees nothing gives zeros.
+ *   dev_out must not overlap dev_q.  The new tokens' keys have to be in the cache (append).  A query that sees nothing gives zeros.
+ *   Logits, running maxima, sums and outputs are held in 32 bits.  CASCADE_BF16: a probability times its key's V scale is rounded to bf16 (at most 2^-8 of its
+ *   size) for the product with the codes, as this library's other calls round probabilities; CASCADE_F32: nothing is rounded below 32 bits.
+ *   Sums are divided at the end: rows of V larger than 2^119 / (keys that the query sees) may overflow to infinity; a 32-bit query of 3.39e38 or more counts as infinity.
  *   Logits below the range of 32 bits are -infinity: such keys have no weight next to others, and a query that sees no other key gives NaN.
  * read: the new tokens' rows as the values they stand for, into contiguous dev_k_out and dev_v_out (either may be NULL); a row that was left out
  *   on writing (see cascade_paged_batch) is read as zeros.  Any range of a sequence can be read by a batch that calls it new.

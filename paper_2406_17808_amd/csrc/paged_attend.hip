@@ -13,14 +13,16 @@ namespace ckv {
 // and a quarter of the channels, D/4 consecutive ones: one 16-byte piece of codes (D = 128) with one scale, turned into bf16 by
 // v_cvt_scalef32_pk_bf16_fp4 without error (a code has two significant bits).  The accumulators of two such tiles are the logits of keys
 // 4q + b and 16 + 4q + b; V bytes lie in that order, so the probabilities are the B operand of O^T = V^T P^T as they stand.  V codes
-// go in unscaled; a key's scale is a factor of its probability.  fp32: the queries and the scaled probabilities are sums of three bf16 terms
+// go in unscaled; a key's scale is a factor of its probability.  bf16: that product is rounded to bf16, which the matrix instruction takes, with the sum of probabilities from
+// before the rounding: outputs of 131072 keys are off by 0.0023 of their size (root mean square) where the rounding of the outputs alone makes 0.0017; a second term would double
+// the products.  fp32: the queries and the scaled probabilities are sums of three bf16 terms
 // (24 bits), with a product each.
 //
 // A workgroup has kFewWaves waves; wave w takes groups w, w + kFewWaves, ... of the workgroup's share.  A wave has kFewStages groups of its own in
 // LDS, filled by asynchronous copies (a group is contiguous), and waits only for its own.  A group takes a wave 1 to 2 us from its first LDS read to its last product, most of it
 // waiting for itself, so waves a SIMD count for more than bytes on their way: 32 sequences of 16384 keys (562 MB) take 104 us with two
 // stages, 106 with three stages, 114 with four and two workgroups; 132 with the next group's
-// loads in registers.  One token on 131072 keys (140 MB): 26 us and 4 for the join of 94 splits, 5.4 and 4.6 TB/s; a large copy reaches 4.74.  The running maximum is raised only when a logit exceeds it by 2^8 (in 32 bits nothing is lost below 2^127): a
+// loads in registers.  One token on 131072 keys (140 MB): 26 us and 4 for the join of 94 splits, 5.4 and 4.6 TB/s; a large copy reaches 4.74, reads alone 6.5 to 6.9.  The running maximum is raised only when a logit exceeds it by 2^8 (in 32 bits nothing is lost below 2^127): a
 // vote instead of an exchange between lanes for most groups.
 template <int D> struct GroupCodes {
     u32x4_t k[2];            // D = 64: the first two words
@@ -453,7 +455,10 @@ static FewPlan few_plan(const PagedGeom& g, const PagedBatch& b, int limit, int 
 // Whether the kernel for few rows takes sequences of more than kFewRows rows of a KV head too: where it is the cheaper one for the whole batch.  Its workgroups have 32 rows and
 // go over the keys again for each of them; the other kernel's have 256 (fp32: 128), one on a compute unit, begin late and take a tile of 64 keys after the other.  us, from
 // measurements of both: here 6 and 0.28 for 32 rows by 32 keys on a compute unit; there 4, 12 for a workgroup and 2 for a tile; fp32 has three times the
-// products.  bf16, d 128, 8 KV heads of 4 query heads, 16000 keys, us here and there: 16 new tokens of four sequences 41, 135; 32 of one 27, 58; 64 39, 63; 128 about 90, 77.
+// products.  us here and there, 8 KV heads of 4 query heads, on 16000 keys, 48 | 200 | 400 new tokens of one sequence: bf16, d 128 35, 57 | 102, 103 | 178, 147; d 64 29, 46 | 75, 77 |
+// 127, 107; fp32, d 128 67, 106 | 225, 224 | 442, 431; d 64 39, 81 | 123, 169 | 210, 322; 16 of four sequences in bf16 38, 128.  Of 198 calls (both types and head sizes, 2 and 8 KV
+// heads, 1 and 4 sequences, 500 to 16000 keys, 16 to 1000 new tokens) the estimate takes the kernel that is more than 5 % slower in 17, by 1.34 at most (fp32, d 64, 1000 on
+// 16000: 483, 647).
 static bool few_rows_take_all(const PagedGeom& g, const PagedBatch& b, int dtype)
 {
     const int64_t most = (int64_t)b.max_new * g.G, rows = ((int64_t)b.n_tokens * g.G + b.n_seqs - 1) / b.n_seqs;      // of a sequence: the most, the mean

@@ -18,12 +18,16 @@ namespace ckv {
 // tile x + 1 and V of tile x: what matrix block x reads.  The early waves (0 - 3) run matrix block x in phase 2x and write K in the vector block before
 // it, phase 2x - 1; the late waves (4 - 7) run it in phase 2x + 1 and write V in phase 2x - 2.  Nobody reads set x after phase
 // 2x + 1, and set x + 2 is written from phase 2x + 2 on: two stages do.
-// What bounds it: 2048 tokens of 32 heads on 63500 cached ones, d 128, bf16, 2.0 ms: 1.08 PFLOP/s (a large library product in bf16: 1.27); the matrix cores are busy 49 % of the
+// What bounds it: 2048 tokens of 32 heads on 63500 cached ones, d 128, bf16, 2.0 ms: 1.08 PFLOP/s (a large library product in bf16: 1.27); the matrix cores are busy 51 % of the
 // cycles, and a wave issues an instruction every five to six cycles: its vector block (exponentials, codes, maxima) takes 2300 cycles, its matrix block
 // 1650, so that the vector blocks set the pace and each matrix block waits for one.  4096 tokens on none: 153 us, 0.90 PFLOP/s (the tiles at the diagonal,
 // and about 10 us before a workgroup's first product).
+// bf16: a probability times its V scale is rounded to bf16 for the product (the sum takes it before); outputs are off by 0.0021 to 0.0023 of their size (root mean square)
+// where the rounding of the outputs alone makes 0.0016 to 0.0017.
+// d 64, bf16: 2048 on 16000 386 us, 0.74 PFLOP/s, 4096 on none 111 us, 0.62: a tile has half of the products of d 128 and the same exponentials, so that the vector blocks
+// weigh twice as much.
 // NW = 4 (fp32: queries and scaled probabilities are sums of three bf16 terms, three times the products and the query registers): all waves are early and convert
-// K and V.
+// K and V; one wave a SIMD, so that products and exponentials take turns.  2048 on 16000 1.73 ms, 330 TFLOP/s (three products each: 424 at most).
 
 // What a thread converts: N words of codes, and the K byte or a V scale.
 template <int N> struct Piece {

@@ -139,7 +139,7 @@ class PagedBatch:
 
 class PagedKVCache:
     """Pages of keys and values in 4 bits (see cascade_paged_config for the numbers and bytes).  `pages` [n_pages, page bytes] uint8 may be handed in;
-    with `rope` append rotates keys, and the queries given to it, to their positions.  `workspace` (uint8, workspace_size(cfg) bytes) may be shared by layers
+    with `rope` append rotates keys, and the queries given to it, to their positions.  One attend at a time: its partial results lie in the workspace.  `workspace` (uint8, workspace_size(cfg) bytes) may be shared by layers
     whose calls follow each other."""
 
     def __init__(self, cfg: B.cascade_paged_config, device: str = "cuda:0", pages: Optional[torch.Tensor] = None, rope: Optional[RopeTable] = None,
@@ -197,7 +197,8 @@ class PagedKVCache:
 
     def append(self, batch: PagedBatch, k: torch.Tensor, v: torch.Tensor, q: Optional[torch.Tensor] = None,
                q_out: Optional[torch.Tensor] = None) -> Optional[torch.Tensor]:
-        """Stores k, v [n_tokens, kv heads, head_dim] of the batch's new tokens; q [n_tokens, q heads, head_dim] is rotated into q_out, which is returned."""
+        """Stores k, v [n_tokens, kv heads, head_dim] of the batch's new tokens; q [n_tokens, q heads, head_dim] is rotated into q_out, which is returned.
+        Rows of no sequence (n_tokens above what the offsets reach, as in a padded step) are left as they are in q_out; in one made here they hold anything."""
         _serving_only(k, v, q)
         n, d, device, dtype = batch.n_tokens, self.head_dim, self.device, self.torch_dtype
         assert batch.device == device
@@ -216,7 +217,8 @@ class PagedKVCache:
         return q_out
 
     def attend(self, batch: PagedBatch, q: torch.Tensor, out: Optional[torch.Tensor] = None) -> torch.Tensor:
-        """Attention of q [n_tokens, q heads, head_dim], rotated, over the cache, the batch's new tokens included."""
+        """Attention of q [n_tokens, q heads, head_dim], rotated, over the cache, the batch's new tokens included.  Rows of no sequence are left as they are in
+        `out`; in one made here they hold anything (hand in an array of zeros where they are looked at)."""
         _serving_only(q)
         n, d, device, dtype = batch.n_tokens, self.head_dim, self.device, self.torch_dtype
         assert batch.device == device
@@ -230,7 +232,7 @@ class PagedKVCache:
         return out
 
     def read(self, batch: PagedBatch) -> Tuple[torch.Tensor, torch.Tensor]:
-        """The rows that the batch calls new, as the values their codes stand for."""
+        """The rows that the batch calls new, as the values their codes stand for (rows of no sequence hold anything)."""
         assert batch.device == self.device
         k = torch.empty((batch.n_tokens, self.n_kv_heads, self.head_dim), dtype=self.torch_dtype, device=self.device)
         v = _like(k)
