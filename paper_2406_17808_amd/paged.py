@@ -78,7 +78,8 @@ def qk_norm_rope(q: torch.Tensor, k: Optional[torch.Tensor] = None, q_weight: Op
     """RMS norm over head_dim of q [tokens, q heads, head_dim] and k [tokens, k heads, head_dim] with the rotation to `positions`
     [tokens] (int32; None: not rotated, as CascadeKVCache takes them) in the same pass.  norm=False rotates only.  Tokens
     of q and k may lie apart (views of a fused projection).  q_out / k_out may be q / k.  For serving: inputs that require a gradient are refused."""
-    _serving_only(q, k, q_weight, k_weight)
+    if q.requires_grad or k is not None and k.requires_grad or q_weight is not None and q_weight.requires_grad or k_weight is not None and k_weight.requires_grad:
+        _serving_only(q, k, q_weight, k_weight)
     device, dtype, (tokens, hq, d) = q.device, q.dtype, q.shape
     assert q.is_cuda and dtype in _TYPES and tokens < 1 << 31, (device, dtype, tokens)
     q_stride, q_out_stride, hk, k_stride, k_out_stride = _rows(q, device, dtype, tokens, hq, d), 0, 0, 0, 0
@@ -171,16 +172,13 @@ class PagedKVCache:
     def workspace_size(cfg: B.cascade_paged_config) -> int:
         return B.cascade_paged_workspace_bytes(cfg) + 256      # the workspace begins at a multiple of 256
 
-    def _used_on(self) -> int:
-        """The current stream as a number.  The allocator is told of each that the cache's arrays are used on, so that they are not handed out again before
-        its work is done, whenever the cache is dropped."""
-        stream = _stream(self.device)
-        if stream not in self._streams:
-            now = torch.cuda.current_stream(self.device)
-            for x in (self.pages, self.workspace) + ((self.rope.table,) if self.rope is not None else ()):
-                x.record_stream(now)
-            self._streams.add(stream)
-        return stream
+    def _first_use(self, stream: int) -> None:
+        """The allocator is told of each stream that the cache's arrays are used on, so that they are not handed out again before its work is done, whenever
+        the cache is dropped."""
+        now = torch.cuda.current_stream(self.device)
+        for x in (self.pages, self.workspace) + ((self.rope.table,) if self.rope is not None else ()):
+            x.record_stream(now)
+        self._streams.add(stream)
 
     def close(self):
         """Ends the context, a structure of the host: nothing is waited for, so that a cache may also be collected while a stream is being captured.
@@ -199,13 +197,17 @@ class PagedKVCache:
                q_out: Optional[torch.Tensor] = None) -> Optional[torch.Tensor]:
         """Stores k, v [n_tokens, kv heads, head_dim] of the batch's new tokens; q [n_tokens, q heads, head_dim] is rotated into q_out, which is returned.
         Rows of no sequence (n_tokens above what the offsets reach, as in a padded step) are left as they are in q_out; in one made here they hold anything."""
-        _serving_only(k, v, q)
+        if k.requires_grad or v.requires_grad or q is not None and q.requires_grad:
+            _serving_only(k, v, q)
         n, d, device, dtype = batch.n_tokens, self.head_dim, self.device, self.torch_dtype
         assert batch.device == device
+        stream = _stream(device)
+        if stream not in self._streams:
+            self._first_use(stream)
         k_stride, v_stride = _rows(k, device, dtype, n, self.n_kv_heads, d), _rows(v, device, dtype, n, self.n_kv_heads, d)
         if q is None:
             assert q_out is None
-            B.cascade_paged_append(self.ctx, batch.c, k.data_ptr(), k_stride, v.data_ptr(), v_stride, 0, 0, 0, self._used_on())
+            B.cascade_paged_append(self.ctx, batch.c, k.data_ptr(), k_stride, v.data_ptr(), v_stride, 0, 0, 0, stream)
             return None
         q_stride = _rows(q, device, dtype, n, self.n_q_heads, d)
         if q_out is None:
@@ -213,22 +215,26 @@ class PagedKVCache:
         else:
             _rows(q_out, device, dtype, n, self.n_q_heads, d)
             assert q_out.is_contiguous()
-        B.cascade_paged_append(self.ctx, batch.c, k.data_ptr(), k_stride, v.data_ptr(), v_stride, q.data_ptr(), q_stride, q_out.data_ptr(), self._used_on())
+        B.cascade_paged_append(self.ctx, batch.c, k.data_ptr(), k_stride, v.data_ptr(), v_stride, q.data_ptr(), q_stride, q_out.data_ptr(), stream)
         return q_out
 
     def attend(self, batch: PagedBatch, q: torch.Tensor, out: Optional[torch.Tensor] = None) -> torch.Tensor:
         """Attention of q [n_tokens, q heads, head_dim], rotated, over the cache, the batch's new tokens included.  Rows of no sequence are left as they are in
         `out`; in one made here they hold anything (hand in an array of zeros where they are looked at)."""
-        _serving_only(q)
+        if q.requires_grad:
+            _serving_only(q)
         n, d, device, dtype = batch.n_tokens, self.head_dim, self.device, self.torch_dtype
         assert batch.device == device
         q_stride = _rows(q, device, dtype, n, self.n_q_heads, d)
+        stream = _stream(device)
+        if stream not in self._streams:
+            self._first_use(stream)
         if out is None:
             out = _like(q)
         else:
             _rows(out, device, dtype, n, self.n_q_heads, d)
             assert out.is_contiguous()
-        B.cascade_paged_attend(self.ctx, batch.c, q.data_ptr(), q_stride, out.data_ptr(), self._used_on())
+        B.cascade_paged_attend(self.ctx, batch.c, q.data_ptr(), q_stride, out.data_ptr(), stream)
         return out
 
     def read(self, batch: PagedBatch) -> Tuple[torch.Tensor, torch.Tensor]:
@@ -236,5 +242,8 @@ class PagedKVCache:
         assert batch.device == self.device
         k = torch.empty((batch.n_tokens, self.n_kv_heads, self.head_dim), dtype=self.torch_dtype, device=self.device)
         v = _like(k)
-        B.cascade_paged_read(self.ctx, batch.c, k.data_ptr(), v.data_ptr(), self._used_on())
+        stream = _stream(self.device)
+        if stream not in self._streams:
+            self._first_use(stream)
+        B.cascade_paged_read(self.ctx, batch.c, k.data_ptr(), v.data_ptr(), stream)
         return k, v
