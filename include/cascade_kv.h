@@ -382,7 +382,7 @@ int cascade_norm_rope(const cascade_norm_rope_args* args, void* stream);
  *      (7 is the largest value that still rounds to 6), stored as the byte e + 127; all zeros: byte 0.
  *   V: a row has the scale s = max|v| / 6 rounded to bf16; values are code * s.
  *   A K block or V row with an infinity or NaN becomes NaN as a whole (exponent byte 255, scale NaN); a V row with s below
- *   2^-100 becomes zero.
+ *   2^-100 becomes zero; numbers from 2.97e38 on may be rounded to an infinity.
  *   What is stored for a token depends on its row and its position alone, not on the call, chunk or kernel that wrote it.
  * Bytes: a page is [n_kv_heads][page_size / 32] groups of 32 tokens of (33 * head_dim + 64) bytes, rounded up to 128.
  * Token r of a group, channel c:
